@@ -194,6 +194,130 @@ int pi_attn_decode_step(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t 
                         void *out, float *lse, void *stream);
 
 /*
+ * Quantised caches -- keys and values as e4m3 codes with a scale for each row.
+ * A row of D elements is held as D codes (OCP e4m3: 4 bits of exponent, 3 of
+ * mantissa, no infinities, largest 448) and one byte b: element d has the value
+ * code_d * 2^(b - 127).  With amax the row's largest finite magnitude, the byte
+ * is that of the least e = b - 127 >= -126 with amax <= 448 * 2^e, and a code is
+ * x_d * 2^-e rounded to the nearest, ties to even: off by at most 2^-4 of the
+ * element, or 2^(e - 10) for elements below 2^(e - 6).  Infinities and NaN are
+ * held as NaN.  Bytes of 1 to 254 are valid.  A cache is two such tables, codes
+ * [S][H][cap][D] and bytes [S][H][cap], for the keys and for the values.
+ *
+ * pi_attn_cache_store -- rows of a prompt, or of a chunk of one, into a
+ * quantised cache: row i < min(count[s], n) of k and v becomes cache row
+ * start[s] + i of every head.
+ *   dtype        PI_ATTN_F32 or PI_ATTN_BF16: element type of k and v.
+ *   S, H, n, cap sequences, heads, rows given for each, cache rows (>= 1).
+ *   k, v         device [S][H][n][D] through element strides (sb, sh, sn)
+ *                shared by both, the D elements contiguous.
+ *   start        device int32 [S], or NULL for 0.
+ *   count        device int32 [S], or NULL for n (negative: none).
+ *   k_cache, v_cache   device codes [S][H][cap][D] contiguous.
+ *   k_exp, v_exp       device bytes [S][H][cap] contiguous.
+ * A row whose place lies outside [0, cap) is dropped; every other row of the
+ * caches is left as it was.  Buffers must not overlap.
+ * Errors: EINVAL (null pointer with rows to store, negative size or stride,
+ * misalignment, S*H*n of 2^31 and more), EUNSUPPORTED (D not 64/128, unknown
+ * dtype), EHIP (launch refused).
+ */
+int pi_attn_cache_store(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t n, int32_t cap,
+                        const void *k, const void *v, int64_t sb, int64_t sh, int64_t sn,
+                        const int32_t *start, const int32_t *count,
+                        void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp, void *stream);
+
+/*
+ * pi_attn_cache_load -- rows of a quantised cache in the working type: row i <
+ * n of k and v is cache row start[s] + i, and zeros where i >= count[s] or that
+ * row lies outside [0, cap).  What it returns can go into pi_attn_forward_shard
+ * as the rows that a later chunk of the prompt attends.
+ *   Arguments    as pi_attn_cache_store; every row of k and v [S][H][n][D] is
+ *                written (through sb, sh, sn, each at least D where its extent
+ *                is more than 1), values rounded to dtype (exact but for
+ *                magnitudes below 2^-126 or past dtype's largest).
+ * Errors: as pi_attn_cache_store.
+ */
+int pi_attn_cache_load(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t n, int32_t cap,
+                       const void *k_cache, const void *v_cache, const uint8_t *k_exp, const uint8_t *v_exp,
+                       const int32_t *start, const int32_t *count,
+                       void *k, void *v, int64_t sb, int64_t sh, int64_t sn, void *stream);
+
+/*
+ * pi_attn_decode_workspace -- float32 elements of workspace that
+ * pi_attn_decode_step_e4m3 (plen = 0) and pi_attn_decode_step_prefix need for
+ * these sizes; 0 if none, -1 for sizes that they refuse.  The contents never
+ * matter between calls; calls that may run at the same time need one each.
+ */
+int64_t pi_attn_decode_workspace(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t plen, int32_t cap,
+                                 int32_t k);
+
+/*
+ * pi_attn_decode_step_e4m3 -- pi_attn_decode_step over quantised caches: the
+ * new row is stored quantised as cache row t = len_in[s] (codes and byte), and
+ * the query attends over W_t with every row as it is stored, the new one too.
+ *   dtype ... v_new, gate ... lse   as pi_attn_decode_step (dtype: of q_new,
+ *                k_new, v_new and out).
+ *   k_cache, v_cache, k_exp, v_exp  a quantised cache; row len_in[s] of every
+ *                head is overwritten, nothing else is written.
+ *   work         device float32, 16-byte aligned, of
+ *                pi_attn_decode_workspace(dtype, S, H, D, 0, cap, k) elements;
+ *                may be NULL when that is 0.
+ * A length outside [0, cap) is answered as in pi_attn_decode_step.  Long
+ * windows of a few (s, h) are split over work-groups, in two launches; the sums
+ * are taken in a fixed order either way.
+ * Errors: as pi_attn_decode_step, plus EINVAL for a null k_exp or v_exp and for
+ * a null or misaligned work that is needed, EUNSUPPORTED for S*H of 2^24 and
+ * more or cap above 2^31 - 4097.
+ */
+int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t cap, int32_t k, int32_t pi,
+                             const int32_t *len_in, int32_t *len_out,
+                             const void *q_new, const void *k_new, const void *v_new,
+                             void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp,
+                             const float *gate, int64_t gss, int64_t gsh, float scale, float logit_clamp,
+                             void *out, float *lse, float *work, void *stream);
+
+/*
+ * pi_attn_decode_step_prefix -- one decode step of a batch of sequences that
+ * begin with the same plen rows: these are held once, and read once a step for
+ * all sequences; each sequence has a cache of its own for the rows behind them.
+ * With t = plen + len_in[s] the step stores the new row as row len_in[s] of the
+ * sequence's own cache and attends over W_t as pi_attn_decode_step does over
+ * one cache that holds the plen rows and then the own ones (window and partner
+ * by position t; positions below plen in the prefix).
+ *   dtype        of q_new, k_new, v_new and out.  All caches, own and shared,
+ *                are in dtype, or (k_exp not NULL) quantised.
+ *   plen         shared rows (>= 0); pcap (>= plen) rows from one head's prefix
+ *                to the next, so that the first rows of one sequence of a
+ *                larger cache can serve as the prefix of others.
+ *   cap          rows of an own cache.
+ *   len_in       device int32 [S]: own rows so far (0 <= len_in[s] < cap).
+ *   k_prefix, v_prefix          device [H][pcap][D] (not read for plen = 0).
+ *   k_prefix_exp, v_prefix_exp  their bytes [H][pcap], NULL unless quantised.
+ *   k_cache, v_cache            device [S][H][cap][D] contiguous; row
+ *                len_in[s] of every head is overwritten, nothing else is
+ *                written.
+ *   k_exp, v_exp                their bytes [S][H][cap], both NULL unless
+ *                quantised.
+ *   k, pi, len_out, q_new, k_new, v_new, gate ... lse   as pi_attn_decode_step.
+ *   work         as pi_attn_decode_step_e4m3, for plen.
+ * A length outside [0, cap): NaN for that sequence's outputs, its caches
+ * untouched, len_out[s] = len_in[s].  bf16: the weights of the prefix rows
+ * enter their value product as bf16.
+ * Errors: as pi_attn_decode_step, plus EINVAL for plen < 0, pcap < plen, some
+ * but not all of the needed byte tables, a null or misaligned k_prefix,
+ * v_prefix (plen > 0) or work that is needed; EUNSUPPORTED for S*H of 2^24 and
+ * more or plen + cap above 2^31 - 4097.
+ */
+int pi_attn_decode_step_prefix(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t plen, int32_t pcap,
+                               int32_t cap, int32_t k, int32_t pi, const int32_t *len_in, int32_t *len_out,
+                               const void *q_new, const void *k_new, const void *v_new,
+                               const void *k_prefix, const void *v_prefix,
+                               const uint8_t *k_prefix_exp, const uint8_t *v_prefix_exp,
+                               void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp,
+                               const float *gate, int64_t gss, int64_t gsh, float scale, float logit_clamp,
+                               void *out, float *lse, float *work, void *stream);
+
+/*
  * pi_attn_backward -- gradients of the full-sequence operator for a loss L
  * given dL/dy (the softmax Jacobian on the fused logits, Sec. 3.5 eq. jac;
  * the prior derivatives for the clipped gate, eqs. ddelta_da and dalpha_da;

@@ -18,6 +18,12 @@ bidirectional mode, window |j - t| <= k and partners t -/+ pi):
     pi_attn_forward_gated(q, k, v, u, w2, b2, k_window, pi)   -> out, gate logits [B,H,N]
     pi_attn_backward(q, k, v, gate, k_window, pi, out, lse, dout, causal=True)
     pi_attn_decode_step(len_in, q_new, k_new, v_new, k_cache, v_cache, gate, k, pi)
+    pi_attn_cache_store(k, v, k_cache, v_cache, k_exp, v_exp, start=None, count=None)
+    pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n, start=None, count=None)   -> k, v [S,H,n,D]
+    pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp, gate, k, pi)
+    pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k, pi)
+Quantised caches are torch.float8_e4m3fn codes [S,H,cap,D] with a torch.uint8
+scale byte for each row [S,H,cap].
 """
 from __future__ import annotations
 
@@ -28,6 +34,8 @@ import threading
 __all__ = ["pi_attn_index_set", "pi_attn_forward", "pi_attn_forward_gated", "pi_attn_backward",
            "pi_attn_backward_noalloc",
            "pi_attn_decode_step", "pi_attn_ws_width",
+           "pi_attn_cache_store", "pi_attn_cache_load", "pi_attn_decode_step_e4m3", "pi_attn_decode_step_prefix",
+           "pi_attn_decode_workspace",
            "pi_attn_forward_shard", "pi_attn_backward_shard_q", "pi_attn_backward_shard_kv",
            "pi_attn_strerror", "library", "LIB_PATH", "EXPORTED_SYMBOLS", "PiAttnError"]
 
@@ -36,7 +44,9 @@ BINDING_PATH = os.path.join(os.path.dirname(LIB_PATH), "_binding.so")
 EXPORTED_SYMBOLS = ("pi_attn_strerror", "pi_attn_ws_width", "pi_attn_default_scale", "pi_attn_index_set",
                     "pi_attn_forward", "pi_attn_forward_gated", "pi_attn_decode_step", "pi_attn_backward",
                     "pi_attn_gate_grad_per_head", "pi_attn_forward_shard", "pi_attn_backward_shard_q",
-                    "pi_attn_backward_shard_kv", "pi_attn_backward_noalloc")
+                    "pi_attn_backward_shard_kv", "pi_attn_backward_noalloc", "pi_attn_cache_store",
+                    "pi_attn_cache_load", "pi_attn_decode_workspace", "pi_attn_decode_step_e4m3",
+                    "pi_attn_decode_step_prefix")
 
 PI_ATTN_F32, PI_ATTN_BF16 = 0, 1
 
@@ -77,6 +87,16 @@ def library() -> ctypes.CDLL:
             lib.pi_attn_decode_step.argtypes = ([i32] * 7 + [vp, vp, vp, vp, vp, vp, vp, vp, i64, i64,
                                                             f32, f32, vp, vp, vp])
             lib.pi_attn_decode_step.restype = ctypes.c_int
+            lib.pi_attn_cache_store.argtypes = [i32] * 6 + [vp, vp, i64, i64, i64] + [vp] * 7
+            lib.pi_attn_cache_store.restype = ctypes.c_int
+            lib.pi_attn_cache_load.argtypes = [i32] * 6 + [vp] * 8 + [i64, i64, i64, vp]
+            lib.pi_attn_cache_load.restype = ctypes.c_int
+            lib.pi_attn_decode_workspace.argtypes = [i32] * 7
+            lib.pi_attn_decode_workspace.restype = i64
+            lib.pi_attn_decode_step_e4m3.argtypes = ([i32] * 7 + [vp] * 10 + [i64, i64, f32, f32, vp, vp, vp, vp])
+            lib.pi_attn_decode_step_e4m3.restype = ctypes.c_int
+            lib.pi_attn_decode_step_prefix.argtypes = ([i32] * 9 + [vp] * 14 + [i64, i64, f32, f32, vp, vp, vp, vp])
+            lib.pi_attn_decode_step_prefix.restype = ctypes.c_int
             lib.pi_attn_backward.argtypes = ([i32] * 8 + [vp, vp, vp, i64, i64, i64, vp, i64, i64, i64,
                                                          f32, f32, vp, vp, vp, i64, i64, i64,
                                                          vp, vp, vp, vp, vp, vp])
@@ -112,6 +132,7 @@ class _PythonOnly:
         return None
 
     forward_gated = backward = decode_step = forward
+    cache_store = cache_load = decode_step_e4m3 = decode_step_prefix = forward
 
 
 def _load_native():
@@ -591,3 +612,244 @@ def pi_attn_decode_step(len_in, q_new, k_new, v_new, k_cache, v_cache, gate, k: 
         float(scale), float(logit_clamp), _ptr(out), _ptr(lse), _stream_handle(stream, q_new.device))
     _check(st, "pi_attn_decode_step")
     return out
+
+
+def _cache_checked(torch, k_cache, v_cache, k_exp, v_exp):
+    """The sizes of a quantised cache."""
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must share one [S, H, cap, D] shape")
+    if k_cache.dtype != torch.float8_e4m3fn or v_cache.dtype != torch.float8_e4m3fn:
+        raise TypeError("quantised caches must be float8_e4m3fn")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("caches must be contiguous")
+    for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+        if t.dtype != torch.uint8 or t.shape != k_cache.shape[:3] or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous uint8 [S, H, cap] tensor")
+    return k_cache.shape
+
+
+def _per_sequence(torch, t, S, name):
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (S,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 [{S}] tensor")
+    return t
+
+
+def _same_device(*ts):
+    devices = {t.device for t in ts if t is not None}
+    if len(devices) > 1:
+        raise ValueError("all tensors must be on one device")
+
+
+def pi_attn_cache_store(k, v, k_cache, v_cache, k_exp, v_exp, start=None, count=None, stream=None):
+    """Stores rows in a quantised cache: row i < min(count[s], n) of k and v
+    [S, H, n, D] (float32 or bfloat16, identical strides, last dimension
+    contiguous) becomes cache row start[s] + i.
+
+    k_cache, v_cache: float8_e4m3fn codes [S, H, cap, D]; k_exp, v_exp: uint8
+    [S, H, cap], the scale 2^(byte - 127) of each row; all contiguous.  start,
+    count: int32 [S] on the GPU (0 and n).  Rows that fall outside the cache are
+    dropped, all others of the cache are left as they were.
+    """
+    r = (_native or _load_native()).cache_store(k, v, k_cache, v_cache, k_exp, v_exp, start, count, stream)
+    if r is not None:
+        return
+    torch = _torch()
+    _require_cuda(k, v, k_cache, v_cache, k_exp, v_exp, start, count)
+    _same_device(k, v, k_cache, v_cache, k_exp, v_exp, start, count)
+    S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+        raise ValueError("k and v must share one [S, H, n, D] shape, dtype and strides")
+    if (k.shape[0], k.shape[1], k.shape[3]) != (S, H, D) or k.stride(3) != 1:
+        raise ValueError(f"k and v must be [{S}, {H}, n, {D}] with a contiguous last dimension")
+    _per_sequence(torch, start, S, "start")
+    _per_sequence(torch, count, S, "count")
+    with torch.cuda.device(k.device):
+        st = library().pi_attn_cache_store(
+            _dtype_code(k.dtype), S, H, D, k.shape[2], cap, _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2),
+            _ptr(start), _ptr(count), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp),
+            _stream_handle(stream, k.device))
+    _check(st, "pi_attn_cache_store")
+
+
+def pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n: int, start=None, count=None, dtype=None, k=None, v=None,
+                       stream=None):
+    """Rows of a quantised cache (see pi_attn_cache_store) in the working type:
+    row i < n of the returned k and v [S, H, n, D] is cache row start[s] + i,
+    and zeros where i >= count[s] or the cache has no such row.  dtype: that of
+    the given outputs, bfloat16 without any; k, v: outputs to write to
+    (identical strides, last dimension contiguous)."""
+    r = (_native or _load_native()).cache_load(k_cache, v_cache, k_exp, v_exp, n, start, count, dtype, k, v, stream)
+    if r is not None:
+        return r
+    torch = _torch()
+    _require_cuda(k_cache, v_cache, k_exp, v_exp, start, count, k, v)
+    _same_device(k_cache, v_cache, k_exp, v_exp, start, count, k, v)
+    S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
+    n = int(n)
+    if n < 0:
+        raise ValueError("n must not be negative")
+    if dtype is None:
+        dtype = torch.bfloat16 if k is None and v is None else (v if k is None else k).dtype
+    if k is None:
+        k = torch.empty((S, H, n, D), dtype=dtype, device=k_cache.device) if v is None else torch.empty_like(v)
+    if v is None:
+        v = torch.empty_like(k)
+    for t in (k, v):
+        if tuple(t.shape) != (S, H, n, D) or t.dtype != dtype or t.stride() != k.stride() or t.stride(3) != 1:
+            raise ValueError(f"k and v must be {dtype} [{S}, {H}, {n}, {D}] tensors that share strides, with a "
+                             "contiguous last dimension")
+    _per_sequence(torch, start, S, "start")
+    _per_sequence(torch, count, S, "count")
+    with torch.cuda.device(k_cache.device):
+        st = library().pi_attn_cache_load(
+            _dtype_code(dtype), S, H, D, n, cap, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(start),
+            _ptr(count), _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2), _stream_handle(stream, k.device))
+    _check(st, "pi_attn_cache_load")
+    return k, v
+
+
+def pi_attn_decode_workspace(dtype, S: int, H: int, D: int, plen: int, cap: int, k: int) -> int:
+    """float32 elements of workspace that a step of pi_attn_decode_step_e4m3
+    (plen = 0) or pi_attn_decode_step_prefix needs."""
+    n = int(library().pi_attn_decode_workspace(_dtype_code(dtype), int(S), int(H), int(D), int(plen), int(cap), int(k)))
+    if n < 0:
+        raise PiAttnError(-1, "pi_attn_decode_workspace")
+    return n
+
+
+def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse):
+    """The arguments that the cached decode steps share; the output and the gate's strides."""
+    for name, t in (("q_new", q_new), ("k_new", k_new), ("v_new", v_new)):
+        if tuple(t.shape) != (S, H, D) or not t.is_contiguous() or t.dtype != q_new.dtype:
+            raise ValueError(f"{name} must be a contiguous [S, H, D] tensor, all three of one dtype")
+    _per_sequence(torch, len_in, S, "len_in")
+    _per_sequence(torch, len_out, S, "len_out")
+    if gate.dtype != torch.float32:
+        raise TypeError("gate logits must be float32")
+    if tuple(gate.shape) == (H,):
+        strides = (0, gate.stride(0))
+    elif tuple(gate.shape) == (S, H):
+        strides = (gate.stride(0), gate.stride(1))
+    else:
+        raise ValueError("decode gate must be [H] or [S, H]")
+    if out is None:
+        out = torch.empty_like(q_new)
+    if tuple(out.shape) != (S, H, D) or out.dtype != q_new.dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous [S, H, D] tensor of q_new's dtype")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (S, H) or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [S, H] tensor")
+    return out, strides
+
+
+def _workspace(torch, work, dtype, S, H, D, plen, cap, k, device):
+    """The caller's workspace (checked), a new one, or None where none is needed."""
+    need = int(library().pi_attn_decode_workspace(_dtype_code(dtype), S, H, D, plen, cap, int(k)))
+    if work is None:
+        return torch.empty(need, dtype=torch.float32, device=device) if need > 0 else None
+    if work.dtype != torch.float32 or not work.is_contiguous() or work.numel() < need:
+        raise ValueError(f"work must be a contiguous float32 tensor of at least {need} elements")
+    return work
+
+
+def pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp, gate, k: int, pi: int,
+                             scale: float | None = None, logit_clamp: float = 0.0, len_out=None, out=None, lse=None,
+                             work=None, stream=None):
+    """One decode step over quantised caches (see pi_attn_cache_store): stores
+    k_new/v_new [S, H, D] quantised as row len_in[s], then attends q_new over
+    W_t with every row as it is stored.  work: a float32 workspace of
+    pi_attn_decode_workspace(q_new.dtype, S, H, D, 0, cap, k) elements, or None
+    to have it allocated.  Returns out [S, H, D] in q_new's dtype."""
+    r = (_native or _load_native()).decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp,
+                                                     gate, k, pi, scale, logit_clamp, len_out, out, lse, work, stream)
+    if r is not None:
+        return r
+    torch = _torch()
+    ts = (len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp, gate, len_out, out, lse, work)
+    _require_cuda(*ts)
+    _same_device(*ts)
+    S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
+    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
+    work = _workspace(torch, work, q_new.dtype, S, H, D, 0, cap, k, q_new.device)
+    with torch.cuda.device(q_new.device):
+        st = library().pi_attn_decode_step_e4m3(
+            _dtype_code(q_new.dtype), S, H, D, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out), _ptr(q_new),
+            _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(gate), gss, gsh,
+            _scale(scale, D), float(logit_clamp), _ptr(out), _ptr(lse), _ptr(work),
+            _stream_handle(stream, q_new.device))
+    _check(st, "pi_attn_decode_step_e4m3")
+    return out
+
+
+def pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k: int,
+                               pi: int, k_prefix_exp=None, v_prefix_exp=None, k_exp=None, v_exp=None,
+                               scale: float | None = None, logit_clamp: float = 0.0, len_out=None, out=None, lse=None,
+                               work=None, stream=None):
+    """One decode step of S sequences that share their first plen rows.
+
+    k_prefix, v_prefix [H, plen, D]: the shared rows, held once; a contiguous
+    tensor or the first plen rows of a longer one ([H, cap, D] cut to
+    [:, :plen], e.g. one sequence of another cache).  k_cache, v_cache
+    [S, H, cap, D]: each sequence's rows behind them, len_in[s] so far; the step
+    stores k_new/v_new [S, H, D] there as row len_in[s] and attends q_new at
+    position plen + len_in[s] over its working set.  All in q_new's dtype, or
+    float8_e4m3fn with the bytes k_prefix_exp, v_prefix_exp [H, plen] and k_exp,
+    v_exp [S, H, cap] (see pi_attn_cache_store).  work: a float32 workspace of
+    pi_attn_decode_workspace(q_new.dtype, S, H, D, plen, cap, k) elements, or
+    None to have it allocated.  Returns out [S, H, D]."""
+    r = (_native or _load_native()).decode_step_prefix(
+        len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k, pi, k_prefix_exp, v_prefix_exp,
+        k_exp, v_exp, scale, logit_clamp, len_out, out, lse, work, stream)
+    if r is not None:
+        return r
+    torch = _torch()
+    ts = (len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k_prefix_exp, v_prefix_exp, k_exp,
+          v_exp, len_out, out, lse, work)
+    _require_cuda(*ts)
+    _same_device(*ts)
+    quantised = k_cache.dtype == torch.float8_e4m3fn
+    bytes_ = (k_prefix_exp, v_prefix_exp, k_exp, v_exp)
+    if any((b is not None) != quantised for b in bytes_):
+        raise ValueError("k_prefix_exp, v_prefix_exp, k_exp and v_exp belong to float8_e4m3fn caches, all four")
+    if quantised:
+        S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
+    else:
+        if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+            raise ValueError("k_cache and v_cache must share one [S, H, cap, D] shape")
+        if k_cache.dtype != q_new.dtype or v_cache.dtype != q_new.dtype:
+            raise TypeError("caches must be in q_new's dtype, or float8_e4m3fn")
+        if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+            raise ValueError("caches must be contiguous")
+        S, H, cap, D = k_cache.shape
+    plen, pcap = _prefix_checked(k_prefix, v_prefix, k_cache.dtype, H, D)
+    if quantised:
+        for name, t in (("k_prefix_exp", k_prefix_exp), ("v_prefix_exp", v_prefix_exp)):
+            if t.dtype != torch.uint8 or tuple(t.shape) != (H, plen) or (
+                    plen > 1 and t.stride(1) != 1 or H > 1 and plen > 0 and t.stride(0) != pcap):
+                raise ValueError(f"{name} must be a uint8 [H, plen] tensor that lies as the rows of k_prefix do")
+    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
+    work = _workspace(torch, work, q_new.dtype, S, H, D, plen, cap, k, q_new.device)
+    with torch.cuda.device(q_new.device):
+        st = library().pi_attn_decode_step_prefix(
+            _dtype_code(q_new.dtype), S, H, D, plen, pcap, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out),
+            _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(k_prefix), _ptr(v_prefix), _ptr(k_prefix_exp),
+            _ptr(v_prefix_exp), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(gate), gss, gsh,
+            _scale(scale, D), float(logit_clamp), _ptr(out), _ptr(lse), _ptr(work),
+            _stream_handle(stream, q_new.device))
+    _check(st, "pi_attn_decode_step_prefix")
+    return out
+
+
+def _prefix_checked(k_prefix, v_prefix, dtype, H, D):
+    """plen, and the rows from one head's prefix to the next."""
+    for name, t in (("k_prefix", k_prefix), ("v_prefix", v_prefix)):
+        if t.dim() != 3 or t.shape != k_prefix.shape or t.shape[0] != H or t.shape[2] != D or t.dtype != dtype:
+            raise ValueError(f"{name} must be a [{H}, plen, {D}] tensor of the caches' dtype")
+        if t.numel() and (t.stride(2) != 1 or t.shape[1] > 1 and t.stride(1) != D or t.stride(0) != k_prefix.stride(0)):
+            raise ValueError("k_prefix and v_prefix must share strides, with a head's rows one after the other")
+    plen = k_prefix.shape[1]
+    if plen == 0 or H <= 1:
+        return plen, plen
+    pcap, rest = divmod(k_prefix.stride(0), D)
+    if rest or pcap < plen:
+        raise ValueError("the heads of k_prefix must lie whole rows apart, at least plen")
+    return plen, pcap

@@ -227,6 +227,95 @@ int prepare_backward(int32_t dtype, int32_t B, int32_t H, int32_t N, int32_t D, 
     return PI_ATTN_OK;
 }
 
+// Validation of a decode step's shared arguments; fills p on PI_ATTN_OK
+// (empty: nothing to do).
+int prepare_decode(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t cap, int32_t k, int32_t pi,
+                   const int32_t *len_in, int32_t *len_out, const void *q_new, const void *k_new, const void *v_new,
+                   void *k_cache, void *v_cache, const float *gate, int64_t gss, int64_t gsh, float scale,
+                   float logit_clamp, void *out, float *lse, DecodeParams &p, bool &empty) {
+    empty = false;
+    if (elem_size(dtype) == 0) return PI_ATTN_EUNSUPPORTED;
+    if (S < 0 || H < 0 || cap < 1 || k < 0 || pi < 0) return PI_ATTN_EINVAL;
+    if (D != 64 && D != 128) return PI_ATTN_EUNSUPPORTED;
+    if (!isfinite(scale) || scale <= 0.0f || isnan(logit_clamp)) return PI_ATTN_EINVAL;
+    const int64_t n = (int64_t)S * H;
+    if (n >= kMaxRows) return PI_ATTN_EINVAL;
+    if (n == 0) {
+        empty = true;
+        return PI_ATTN_OK;
+    }
+    if (!len_in || !q_new || !k_new || !v_new || !k_cache || !v_cache || !gate || !out) return PI_ATTN_EINVAL;
+    if (len_out) {   // len_out must not overlap len_in: other work-groups of the step still read it
+        const uintptr_t a = reinterpret_cast<uintptr_t>(len_in), b = reinterpret_cast<uintptr_t>(len_out);
+        const uintptr_t bytes = (uintptr_t)S * sizeof(int32_t);
+        if (a < b + bytes && b < a + bytes) return PI_ATTN_EINVAL;
+    }
+    if (!aligned4(len_in) || (len_out && !aligned4(len_out))) return PI_ATTN_EINVAL;
+    if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) ||
+        !aligned16(v_cache) || !aligned16(out))
+        return PI_ATTN_EINVAL;
+    if (!aligned4(gate) || gss < 0 || gsh < 0) return PI_ATTN_EINVAL;
+    if (lse && !aligned4(lse)) return PI_ATTN_EINVAL;
+    p.S = S; p.H = H; p.D = D; p.cap = cap; p.k = k; p.pi = pi;
+    p.len_in = len_in; p.len_out = len_out;
+    p.q_new = q_new; p.k_new = k_new; p.v_new = v_new;
+    p.k_cache = k_cache; p.v_cache = v_cache;
+    p.gate = gate; p.gss = gss; p.gsh = gsh;
+    p.scale = scale;
+    p.clamp = logit_clamp > 0.0f ? logit_clamp : 0.0f;
+    p.out = out; p.lse = lse;
+    return PI_ATTN_OK;
+}
+
+// Sizes that the cached steps' kernels index with 32 bits: positions (with a
+// tile's rows to spare), and a work-group for each (s, h).
+bool cached_sizes_ok(int32_t S, int32_t H, int32_t plen, int32_t cap) {
+    return (int64_t)plen + cap <= INT32_MAX - 4096 && (int64_t)S * H < ((int64_t)1 << 24);
+}
+
+int64_t part_rows(const CachedParams &p) { return (int64_t)(p.chunks + p.own_parts) * p.d.S * p.d.H; }
+
+// The rest of a cached step whose arguments p holds: sizes, workspace, launch.
+int decode_cached(CachedParams &p, int32_t dtype, float *work, void *stream) {
+    if (!cached_sizes_ok(p.d.S, p.d.H, p.plen, p.d.cap)) return PI_ATTN_EUNSUPPORTED;
+    const bool bf16 = dtype == PI_ATTN_BF16;
+    plan_decode_cached(p, bf16);
+    const int64_t rows = part_rows(p);
+    if (rows > 0 && (!work || !aligned16(work))) return PI_ATTN_EINVAL;
+    p.part_o = work;
+    p.part_ml = work + rows * p.d.D;
+    return from_hip(launch_decode_cached(p, bf16, (hipStream_t)stream));
+}
+
+// Both directions between rows in the working type and a quantised cache.
+int cache_rows(bool store, int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t n, int32_t cap, void *k, void *v,
+               int64_t sb, int64_t sh, int64_t sn, const int32_t *start, const int32_t *count, void *k_cache,
+               void *v_cache, uint8_t *k_exp, uint8_t *v_exp, void *stream) {
+    const int es = elem_size(dtype);
+    if (es == 0) return PI_ATTN_EUNSUPPORTED;
+    if (S < 0 || H < 0 || n < 0 || cap < 1) return PI_ATTN_EINVAL;
+    if (D != 64 && D != 128) return PI_ATTN_EUNSUPPORTED;
+    const int64_t rows = (int64_t)S * H * n;
+    if ((int64_t)S * H >= kMaxRows || rows >= kMaxRows) return PI_ATTN_EINVAL;
+    if (rows == 0) return PI_ATTN_OK;
+    if (!k || !v || !k_cache || !v_cache || !k_exp || !v_exp) return PI_ATTN_EINVAL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache)) return PI_ATTN_EINVAL;
+    if (!stride16(sb, es) || !stride16(sh, es) || !stride16(sn, es)) return PI_ATTN_EINVAL;
+    if ((start && !aligned4(start)) || (count && !aligned4(count))) return PI_ATTN_EINVAL;
+    // rows that a load writes lie apart
+    if (!store && ((S > 1 && sb < D) || (H > 1 && sh < D) || (n > 1 && sn < D))) return PI_ATTN_EINVAL;
+    CacheRowsParams p{};
+    p.S = S; p.H = H; p.n = n; p.D = D; p.cap = cap;
+    p.rows = (uint32_t)rows;
+    p.by_n = Divisor(n);
+    p.by_h = Divisor(H);
+    p.k = k; p.v = v; p.sb = sb; p.sh = sh; p.sn = sn;
+    p.start = start; p.count = count;
+    p.k_cache = (uint8_t *)k_cache; p.v_cache = (uint8_t *)v_cache;
+    p.k_exp = k_exp; p.v_exp = v_exp;
+    return from_hip(launch_cache_rows(p, store, dtype == PI_ATTN_BF16, (hipStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -270,38 +359,80 @@ int pi_attn_decode_step(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t 
                         const int32_t *len_in, int32_t *len_out, const void *q_new, const void *k_new,
                         const void *v_new, void *k_cache, void *v_cache, const float *gate, int64_t gss,
                         int64_t gsh, float scale, float logit_clamp, void *out, float *lse, void *stream) {
-    const int es = elem_size(dtype);
-    if (es == 0) return PI_ATTN_EUNSUPPORTED;
-    if (S < 0 || H < 0 || cap < 1 || k < 0 || pi < 0) return PI_ATTN_EINVAL;
-    if (D != 64 && D != 128) return PI_ATTN_EUNSUPPORTED;
-    if (!isfinite(scale) || scale <= 0.0f || isnan(logit_clamp)) return PI_ATTN_EINVAL;
-    const int64_t n = (int64_t)S * H;
-    if (n >= kMaxRows) return PI_ATTN_EINVAL;
-    if (n == 0) return PI_ATTN_OK;
-    if (!len_in || !q_new || !k_new || !v_new || !k_cache || !v_cache || !gate || !out) return PI_ATTN_EINVAL;
-    if (len_out) {   // len_out must not overlap len_in: other work-groups of the step still read it
-        const uintptr_t a = reinterpret_cast<uintptr_t>(len_in), b = reinterpret_cast<uintptr_t>(len_out);
-        const uintptr_t bytes = (uintptr_t)S * sizeof(int32_t);
-        if (a < b + bytes && b < a + bytes) return PI_ATTN_EINVAL;
-    }
-    if (!aligned4(len_in) || (len_out && !aligned4(len_out))) return PI_ATTN_EINVAL;
-    if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) ||
-        !aligned16(v_cache) || !aligned16(out))
-        return PI_ATTN_EINVAL;
-    if (!aligned4(gate) || gss < 0 || gsh < 0) return PI_ATTN_EINVAL;
-    if (lse && !aligned4(lse)) return PI_ATTN_EINVAL;
+    DecodeParams p{};
+    bool empty;
+    const int status = prepare_decode(dtype, S, H, D, cap, k, pi, len_in, len_out, q_new, k_new, v_new, k_cache,
+                                      v_cache, gate, gss, gsh, scale, logit_clamp, out, lse, p, empty);
+    if (status != PI_ATTN_OK || empty) return status;
+    return from_hip(launch_decode(p, dtype == PI_ATTN_BF16, (hipStream_t)stream));
+}
 
-    DecodeParams p{};   // decode is causal
-    p.S = S; p.H = H; p.D = D; p.cap = cap; p.k = k; p.pi = pi;
-    p.len_in = len_in; p.len_out = len_out;
-    p.q_new = q_new; p.k_new = k_new; p.v_new = v_new;
-    p.k_cache = k_cache; p.v_cache = v_cache;
-    p.gate = gate; p.gss = gss; p.gsh = gsh;
-    p.scale = scale;
-    p.clamp = logit_clamp > 0.0f ? logit_clamp : 0.0f;
-    p.out = out; p.lse = lse;
-    const hipStream_t st = (hipStream_t)stream;
-    return from_hip(launch_decode(p, dtype == PI_ATTN_BF16, st));
+int pi_attn_cache_store(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t n, int32_t cap, const void *k,
+                        const void *v, int64_t sb, int64_t sh, int64_t sn, const int32_t *start,
+                        const int32_t *count, void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp,
+                        void *stream) {
+    return cache_rows(true, dtype, S, H, D, n, cap, const_cast<void *>(k), const_cast<void *>(v), sb, sh, sn, start,
+                      count, k_cache, v_cache, k_exp, v_exp, stream);
+}
+
+int pi_attn_cache_load(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t n, int32_t cap, const void *k_cache,
+                       const void *v_cache, const uint8_t *k_exp, const uint8_t *v_exp, const int32_t *start,
+                       const int32_t *count, void *k, void *v, int64_t sb, int64_t sh, int64_t sn, void *stream) {
+    return cache_rows(false, dtype, S, H, D, n, cap, k, v, sb, sh, sn, start, count, const_cast<void *>(k_cache),
+                      const_cast<void *>(v_cache), const_cast<uint8_t *>(k_exp), const_cast<uint8_t *>(v_exp),
+                      stream);
+}
+
+int64_t pi_attn_decode_workspace(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t plen, int32_t cap,
+                                 int32_t k) {
+    if (elem_size(dtype) == 0 || S < 0 || H < 0 || cap < 1 || k < 0 || plen < 0) return -1;
+    if ((D != 64 && D != 128) || !cached_sizes_ok(S, H, plen, cap)) return -1;
+    if ((int64_t)S * H == 0) return 0;
+    CachedParams p{};
+    p.d.S = S; p.d.H = H; p.d.D = D; p.d.cap = cap; p.d.k = k; p.plen = plen;
+    plan_decode_cached(p, dtype == PI_ATTN_BF16);
+    return part_rows(p) * (D + 2);
+}
+
+int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t cap, int32_t k, int32_t pi,
+                             const int32_t *len_in, int32_t *len_out, const void *q_new, const void *k_new,
+                             const void *v_new, void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp,
+                             const float *gate, int64_t gss, int64_t gsh, float scale, float logit_clamp, void *out,
+                             float *lse, float *work, void *stream) {
+    CachedParams p{};
+    bool empty;
+    const int status = prepare_decode(dtype, S, H, D, cap, k, pi, len_in, len_out, q_new, k_new, v_new, k_cache,
+                                      v_cache, gate, gss, gsh, scale, logit_clamp, out, lse, p.d, empty);
+    if (status != PI_ATTN_OK || empty) return status;
+    if (!k_exp || !v_exp) return PI_ATTN_EINVAL;
+    p.k_exp = k_exp; p.v_exp = v_exp;
+    return decode_cached(p, dtype, work, stream);
+}
+
+int pi_attn_decode_step_prefix(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t plen, int32_t pcap,
+                               int32_t cap, int32_t k, int32_t pi, const int32_t *len_in, int32_t *len_out,
+                               const void *q_new, const void *k_new, const void *v_new, const void *k_prefix,
+                               const void *v_prefix, const uint8_t *k_prefix_exp, const uint8_t *v_prefix_exp,
+                               void *k_cache, void *v_cache, uint8_t *k_exp, uint8_t *v_exp, const float *gate,
+                               int64_t gss, int64_t gsh, float scale, float logit_clamp, void *out, float *lse,
+                               float *work, void *stream) {
+    if (plen < 0 || pcap < plen) return PI_ATTN_EINVAL;
+    CachedParams p{};
+    bool empty;
+    const int status = prepare_decode(dtype, S, H, D, cap, k, pi, len_in, len_out, q_new, k_new, v_new, k_cache,
+                                      v_cache, gate, gss, gsh, scale, logit_clamp, out, lse, p.d, empty);
+    if (status != PI_ATTN_OK || empty) return status;
+    const bool quantised = k_exp != nullptr;
+    if ((v_exp != nullptr) != quantised) return PI_ATTN_EINVAL;
+    if (plen > 0) {
+        if (!k_prefix || !v_prefix || !aligned16(k_prefix) || !aligned16(v_prefix)) return PI_ATTN_EINVAL;
+        if ((k_prefix_exp != nullptr) != quantised || (v_prefix_exp != nullptr) != quantised) return PI_ATTN_EINVAL;
+    }
+    p.k_exp = k_exp; p.v_exp = v_exp;
+    p.plen = plen; p.pcap = pcap;
+    p.k_prefix = k_prefix; p.v_prefix = v_prefix;
+    p.k_prefix_exp = k_prefix_exp; p.v_prefix_exp = v_prefix_exp;
+    return decode_cached(p, dtype, work, stream);
 }
 
 int pi_attn_forward_shard(int32_t dtype, int32_t B, int32_t H, int32_t D, int32_t k, int32_t pi, int32_t causal,

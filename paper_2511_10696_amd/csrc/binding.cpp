@@ -15,12 +15,14 @@
 // enqueued, and the Python code handles the call (and words the error).  A
 // launch that the HIP runtime refuses (PI_ATTN_EHIP) raises PiAttnError here:
 // of a call of several launches the first ones may be enqueued by then.
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 
@@ -342,6 +344,222 @@ PyObject *decode_step(PyObject *self, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// A quantised cache: codes [S, H, cap, D] and bytes [S, H, cap], no empty extent.
+struct Cache {
+    Tensor k, v, ke, ve;
+    int64_t S, H, cap, D;
+};
+
+bool bytes_ok(const Tensor &t, at::IntArrayRef shape) {
+    return t.scalar_type() == at::kByte && t.sizes() == shape && t.is_contiguous();
+}
+
+// The tables' type and layout; `rows`: the type of codes or of plain rows.
+bool cache_ok(Cache &c, at::ScalarType rows) {
+    if (c.k.dim() != 4 || c.k.scalar_type() != rows || c.v.scalar_type() != rows || c.k.numel() == 0) return false;
+    if (c.v.sizes() != c.k.sizes() || !c.k.is_contiguous() || !c.v.is_contiguous()) return false;
+    c.S = c.k.size(0), c.H = c.k.size(1), c.cap = c.k.size(2), c.D = c.k.size(3);
+    if (c.S > INT32_MAX || c.H > INT32_MAX || c.cap > INT32_MAX || c.D > INT32_MAX) return false;
+    const bool quantised = rows == at::kFloat8_e4m3fn;
+    if (c.ke.defined() != quantised || c.ve.defined() != quantised) return false;
+    const std::array<int64_t, 3> table{c.S, c.H, c.cap};
+    return !quantised || (bytes_ok(c.ke, table) && bytes_ok(c.ve, table));
+}
+
+bool per_sequence(const Tensor &t, int64_t S) {
+    return !t.defined() || (t.scalar_type() == at::kInt && t.dim() == 1 && t.size(0) == S && t.is_contiguous());
+}
+
+// k, v [S, H, n, D] of a cache's rows.
+bool rows_ok(const Tensor &k, const Tensor &v, const Cache &c) {
+    return k.dim() == 4 && dtype_of(k) >= 0 && v.scalar_type() == k.scalar_type() && same_layout(k, v) &&
+           k.size(0) == c.S && k.size(1) == c.H && k.size(3) == c.D && k.stride(3) == 1 && k.size(2) <= INT32_MAX;
+}
+
+// k, v, k_cache, v_cache, k_exp, v_exp, start, count, stream
+PyObject *cache_store(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 9);
+    Cache c;
+    const Tensor k = a.tensor(), v = a.tensor();
+    c.k = a.tensor(), c.v = a.tensor(), c.ke = a.tensor(), c.ve = a.tensor();
+    const Tensor start = a.tensor(true), count = a.tensor(true);
+    a.none();
+    if (!a.ok || !cache_ok(c, at::kFloat8_e4m3fn) || !rows_ok(k, v, c) || !per_sequence(start, c.S) ||
+        !per_sequence(count, c.S))
+        Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        status = pi_attn_cache_store(dtype_of(k), c.S, c.H, c.D, k.size(2), c.cap, k.data_ptr(), v.data_ptr(),
+                                     k.stride(0), k.stride(1), k.stride(2), ptr<int32_t>(start), ptr<int32_t>(count),
+                                     c.k.data_ptr(), c.v.data_ptr(), ptr<uint8_t>(c.ke), ptr<uint8_t>(c.ve),
+                                     stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_cache_store");
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// k_cache, v_cache, k_exp, v_exp, n, start, count, dtype, k, v, stream
+PyObject *cache_load(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 11);
+    Cache c;
+    c.k = a.tensor(), c.v = a.tensor(), c.ke = a.tensor(), c.ve = a.tensor();
+    const int32_t rows = a.integer();
+    const Tensor start = a.tensor(true), count = a.tensor(true);
+    PyObject *dtype = a.next();
+    Tensor k = a.tensor(true), v = a.tensor(true);
+    a.none();
+    if (!a.ok || rows < 1 || !cache_ok(c, at::kFloat8_e4m3fn) || !per_sequence(start, c.S) ||
+        !per_sequence(count, c.S) || k.defined() != v.defined())
+        Py_RETURN_NONE;
+    if (dtype != Py_None && !THPDtype_Check(dtype)) Py_RETURN_NONE;
+    const at::ScalarType want = dtype != Py_None ? reinterpret_cast<THPDtype *>(dtype)->scalar_type
+                                : k.defined()    ? k.scalar_type()
+                                                 : at::kBFloat16;
+    if (want != at::kFloat && want != at::kBFloat16) Py_RETURN_NONE;
+    if (k.defined() && (k.scalar_type() != want || !rows_ok(k, v, c) || k.size(2) != rows)) Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        if (!k.defined()) {
+            const std::array<int64_t, 4> shape{c.S, c.H, rows, c.D};
+            const auto options = at::TensorOptions().dtype(want).device(a.device);
+            k = at::empty(shape, options);
+            v = at::empty(shape, options);
+        }
+        status = pi_attn_cache_load(dtype_of(k), c.S, c.H, c.D, rows, c.cap, c.k.data_ptr(), c.v.data_ptr(),
+                                    ptr<uint8_t>(c.ke), ptr<uint8_t>(c.ve), ptr<int32_t>(start), ptr<int32_t>(count),
+                                    k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                    stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_cache_load");
+    return pack({k, v});
+    END_HANDLE_TH_ERRORS
+}
+
+// The arguments of a decode step but for its caches.
+struct Step {
+    Tensor len_in, q, k, v, gate, len_out, out, lse, work;
+    int64_t gss, gsh;
+};
+
+// What both cached steps check of them, for caches of S, H, cap, D; allocates
+// the output and the workspace where none is given.
+bool step_ok(Step &s, const Cache &c, int64_t plen, int32_t kw, const c10::Device &device) {
+    const std::array<int64_t, 3> rows{c.S, c.H, c.D};
+    const int32_t dt = dtype_of(s.q);
+    const auto fits = [&](const Tensor &t) {
+        return t.scalar_type() == s.q.scalar_type() && t.sizes() == at::IntArrayRef(rows) && t.is_contiguous();
+    };
+    if (dt < 0 || !fits(s.q) || !fits(s.k) || !fits(s.v)) return false;
+    if (!per_sequence(s.len_in, c.S) || !per_sequence(s.len_out, c.S) || s.gate.scalar_type() != at::kFloat) return false;
+    if (s.gate.dim() == 1 && s.gate.size(0) == c.H) {
+        s.gss = 0;
+        s.gsh = s.gate.stride(0);
+    } else if (s.gate.dim() == 2 && s.gate.size(0) == c.S && s.gate.size(1) == c.H) {
+        s.gss = s.gate.stride(0);
+        s.gsh = s.gate.stride(1);
+    } else {
+        return false;
+    }
+    if ((s.out.defined() && !fits(s.out)) || (s.lse.defined() && !is_f32(s.lse, {c.S, c.H}))) return false;
+    const int64_t need = pi_attn_decode_workspace(dt, c.S, c.H, c.D, plen, c.cap, kw);
+    if (need < 0) return false;
+    if (s.work.defined()) {
+        if (s.work.scalar_type() != at::kFloat || !s.work.is_contiguous() || s.work.numel() < need) return false;
+    } else if (need > 0) {
+        s.work = at::empty({need}, at::TensorOptions().dtype(at::kFloat).device(device));
+    }
+    if (!s.out.defined()) s.out = at::empty(rows, at::TensorOptions().dtype(s.q.scalar_type()).device(device));
+    return true;
+}
+
+// len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp, gate, k, pi, scale, logit_clamp, len_out, out, lse, work,
+// stream
+PyObject *decode_step_e4m3(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 18);
+    Step s;
+    Cache c;
+    s.len_in = a.tensor(), s.q = a.tensor(), s.k = a.tensor(), s.v = a.tensor();
+    c.k = a.tensor(), c.v = a.tensor(), c.ke = a.tensor(), c.ve = a.tensor();
+    s.gate = a.tensor();
+    const int32_t kw = a.integer(), pi = a.integer();
+    if (!a.ok || !cache_ok(c, at::kFloat8_e4m3fn)) Py_RETURN_NONE;
+    const float scale = a.real(pi_attn_default_scale((int32_t)c.D)), clamp = a.real(NAN);
+    s.len_out = a.tensor(true), s.out = a.tensor(true), s.lse = a.tensor(true), s.work = a.tensor(true);
+    a.none();
+    if (!a.ok) Py_RETURN_NONE;
+    int status = PI_ATTN_EINVAL;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        if (step_ok(s, c, 0, kw, a.device))
+            status = pi_attn_decode_step_e4m3(dtype_of(s.q), c.S, c.H, c.D, c.cap, kw, pi, ptr<int32_t>(s.len_in),
+                                              ptr<int32_t>(s.len_out), s.q.data_ptr(), s.k.data_ptr(), s.v.data_ptr(),
+                                              c.k.data_ptr(), c.v.data_ptr(), ptr<uint8_t>(c.ke), ptr<uint8_t>(c.ve),
+                                              ptr<float>(s.gate), s.gss, s.gsh, scale, clamp, s.out.data_ptr(),
+                                              ptr<float>(s.lse), ptr<float>(s.work), stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_decode_step_e4m3");
+    return THPVariable_Wrap(s.out);
+    END_HANDLE_TH_ERRORS
+}
+
+// len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k, pi, k_prefix_exp, v_prefix_exp, k_exp,
+// v_exp, scale, logit_clamp, len_out, out, lse, work, stream
+PyObject *decode_step_prefix(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 22);
+    Step s;
+    Cache c;
+    s.len_in = a.tensor(), s.q = a.tensor(), s.k = a.tensor(), s.v = a.tensor();
+    const Tensor kp = a.tensor(), vp = a.tensor();
+    c.k = a.tensor(), c.v = a.tensor();
+    s.gate = a.tensor();
+    const int32_t kw = a.integer(), pi = a.integer();
+    const Tensor kpe = a.tensor(true), vpe = a.tensor(true);
+    c.ke = a.tensor(true), c.ve = a.tensor(true);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::ScalarType rows = c.ke.defined() ? at::kFloat8_e4m3fn : s.q.scalar_type();
+    if (!cache_ok(c, rows)) Py_RETURN_NONE;
+    const float scale = a.real(pi_attn_default_scale((int32_t)c.D)), clamp = a.real(NAN);
+    s.len_out = a.tensor(true), s.out = a.tensor(true), s.lse = a.tensor(true), s.work = a.tensor(true);
+    a.none();
+    if (!a.ok || kp.dim() != 3 || kp.scalar_type() != rows || vp.scalar_type() != rows || !same_layout(kp, vp))
+        Py_RETURN_NONE;
+    const int64_t plen = kp.size(1), pcap = c.H > 1 ? kp.stride(0) / c.D : plen;
+    if (kp.size(0) != c.H || kp.size(2) != c.D || plen < 1 || kp.stride(2) != 1 || (plen > 1 && kp.stride(1) != c.D) ||
+        (c.H > 1 && kp.stride(0) % c.D != 0) || pcap < plen || pcap > INT32_MAX)
+        Py_RETURN_NONE;
+    if (kpe.defined() != c.ke.defined() || vpe.defined() != c.ke.defined()) Py_RETURN_NONE;
+    for (const Tensor &t : {kpe, vpe}) {
+        if (t.defined() && (t.scalar_type() != at::kByte || t.dim() != 2 || t.size(0) != c.H || t.size(1) != plen ||
+                            (plen > 1 && t.stride(1) != 1) || (c.H > 1 && t.stride(0) != pcap)))
+            Py_RETURN_NONE;
+    }
+    int status = PI_ATTN_EINVAL;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        if (step_ok(s, c, plen, kw, a.device))
+            status = pi_attn_decode_step_prefix(
+                dtype_of(s.q), c.S, c.H, c.D, plen, pcap, c.cap, kw, pi, ptr<int32_t>(s.len_in),
+                ptr<int32_t>(s.len_out), s.q.data_ptr(), s.k.data_ptr(), s.v.data_ptr(), kp.data_ptr(), vp.data_ptr(),
+                ptr<uint8_t>(kpe), ptr<uint8_t>(vpe), c.k.data_ptr(), c.v.data_ptr(), ptr<uint8_t>(c.ke),
+                ptr<uint8_t>(c.ve), ptr<float>(s.gate), s.gss, s.gsh, scale, clamp, s.out.data_ptr(),
+                ptr<float>(s.lse), ptr<float>(s.work), stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_decode_step_prefix");
+    return THPVariable_Wrap(s.out);
+    END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction fast(F f) {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -351,6 +569,10 @@ PyMethodDef methods[] = {{"forward", fast(forward), METH_FASTCALL, nullptr},
                          {"forward_gated", fast(forward_gated), METH_FASTCALL, nullptr},
                          {"backward", fast(backward), METH_FASTCALL, nullptr},
                          {"decode_step", fast(decode_step), METH_FASTCALL, nullptr},
+                         {"cache_store", fast(cache_store), METH_FASTCALL, nullptr},
+                         {"cache_load", fast(cache_load), METH_FASTCALL, nullptr},
+                         {"decode_step_e4m3", fast(decode_step_e4m3), METH_FASTCALL, nullptr},
+                         {"decode_step_prefix", fast(decode_step_prefix), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

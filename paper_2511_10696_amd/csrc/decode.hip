@@ -28,57 +28,13 @@
 // 379 -> 167 us at 64.
 #include <algorithm>
 
+#include "decode_rows.h"
 #include "kernels.h"
 #include "pi_common.h"
 
 namespace pi_attn {
 
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-template <typename T, int D>
-struct Row {
-    static constexpr int EPL = 16 / (int)sizeof(T);   // elements per lane
-    static constexpr int LPR = D / EPL;               // lanes per row
-    static constexpr int RPI = 64 / LPR;              // rows per load instruction
-};
-
-typedef unsigned raw16 __attribute__((ext_vector_type(4)));
-
-__device__ inline uint4 ld16(const void *p) { return *reinterpret_cast<const uint4 *>(p); }
-
-// A window row's load that does not keep the row in the caches.
-__device__ inline uint4 ld16_once(const void *p) {
-    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const raw16 *>(p)));
-}
-
-template <typename T>
-__device__ inline void to_f32(uint4 u, float (&f)[16 / sizeof(T)]) {
-    if constexpr (sizeof(T) == 2) {
-        const bf16x8 b = __builtin_bit_cast(bf16x8, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)b[i];
-    } else {
-        const f32x4 b = __builtin_bit_cast(f32x4, u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = b[i];
-    }
-}
-
-// Sum over the LPR lanes of a row, left in each of them: xor 1 and 2 inside
-// quads, the mirrored half-row (8 lanes), the mirrored row (16), then the
-// neighbouring row (32).
-template <int LPR>
-__device__ inline float row_sum(float x) {
-    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, false));
-    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, false));
-    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, false));
-    if constexpr (LPR >= 16) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xF, 0xF, false));
-    if constexpr (LPR >= 32) x += __shfl_xor(x, 16);
-    return x;
-}
 
 // CH: load instructions per chunk; ONCE: window rows are not kept in the caches;
 // PACED: with few of a wavefront's loads in flight at a time.

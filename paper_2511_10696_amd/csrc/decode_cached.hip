@@ -1,0 +1,403 @@
+// decode_cached.hip -- the decode step over quantised caches and the one behind
+// a shared prefix: causal pi-Attention of one new row a sequence, caches in the
+// working type (float32 or bf16) or e4m3 (e4m3.h), fp32 arithmetic, D = 64 or
+// 128.
+//
+// With t = plen + len_in[s], the working set W_t (Sec. 3.5, eq. online_ws) is
+// the window's rows max(0, t - k)..t - 1, the partner t - pi and the new row,
+// which is appended to the sequence's own cache (quantised first, and attended
+// as it is stored).  Rows below plen lie in the prefix, the others in the own
+// cache.  The softmax is joined from parts: the prefix rows of the windows are
+// taken chunk by chunk for all sequences at once (prefix_rows.hip), each chunk
+// leaving (max, sum, weighted values) for every sequence and head; one
+// work-group per (s, h) here takes the own rows, the partner and the new row,
+// and the parts like rows whose weight is the part's sum.
+//
+// Own rows as in decode.hip: 16 bytes a lane, so a load instruction reads 1 KiB
+// of whole rows, CH of them of keys and of values in flight in each wavefront.
+// A quantised row's scale moves into its score and into its weight, both exact
+// (powers of two); codes become floats two an instruction.
+//
+// Few (s, h) with long windows: a work-group per range of own rows, each
+// leaving a part, and a last launch that joins them.
+#include <algorithm>
+
+#include "decode_rows.h"
+#include "e4m3.h"
+#include "kernels.h"
+#include "pi_common.h"
+
+namespace pi_attn {
+
+namespace {
+
+template <typename ST>
+constexpr bool kQuantised = false;
+template <>
+constexpr bool kQuantised<e4m3> = true;
+
+// What a lane holds of a row.
+template <typename ST, int EPL>
+__device__ inline void unpack(uint4 u, float (&f)[EPL]) {
+    if constexpr (kQuantised<ST>) {
+        e4m3_unpack4(u.x, f);
+        e4m3_unpack4(u.y, f + 4);
+        e4m3_unpack4(u.z, f + 8);
+        e4m3_unpack4(u.w, f + 12);
+    } else {
+        to_f32<ST>(u, f);
+    }
+}
+
+// EPL consecutive elements of a row in the working type.
+template <typename T, int EPL>
+__device__ inline void load_wide(const T *p, float (&f)[EPL]) {
+    constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < EPL / N; ++i) {
+        float x[N];
+        to_f32<T>(ld16(p + i * N), x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[i * N + e] = x[e];
+    }
+}
+
+// A new row in the caches' type: the lane's codes, and the row's byte.
+template <int LPR>
+__device__ inline uint4 quantise16(const float (&x)[16], unsigned &byte) {
+    unsigned a = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) a = max(a, finite_bits(x[e]));
+    byte = e4m3_byte(row_max<LPR>(a));
+    const float inv = e4m3_inverse(byte);
+    return make_uint4(e4m3_pack4(x, inv), e4m3_pack4(x + 4, inv), e4m3_pack4(x + 8, inv), e4m3_pack4(x + 12, inv));
+}
+
+// What a launch does of a step: all of it, one range of own rows (a part), or
+// the join of the parts.
+enum { WHOLE, RANGE, JOIN };
+
+template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH, bool ONCE>
+__global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams p) {
+    using R = Row<ST, D>;
+    constexpr bool Q = kQuantised<ST>;
+    constexpr int LPR = R::LPR, RPI = R::RPI, EPL = R::EPL;
+    constexpr int RPC = RPI * CH;   // rows per chunk
+
+    __shared__ float s_m[WAVES], s_l[WAVES];
+    __shared__ float s_acc[WAVES][D];
+
+    const DecodeParams &d = p.d;
+    const DivMod range_of = divmod(blockIdx.x, MODE == RANGE ? p.own_parts : 1);
+    const int64_t sh = range_of.quot;
+    const int range = (int)range_of.rem;
+    const DivMod head_of = divmod(range_of.quot, d.H);
+    const int s = (int)head_of.quot, h = (int)head_of.rem;
+    const int64_t n_sh = (int64_t)d.S * d.H;
+    const int tid = threadIdx.x, lane = __lane_id();
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int sub = lane % LPR, rg = lane / LPR;
+    const int n = d.len_in[s];   // own rows
+    T *out = (T *)d.out + sh * D;
+
+    if (n < 0 || n >= d.cap) {
+        if (MODE == RANGE) return;
+        for (int i = tid; i < D; i += 64 * WAVES) out[i] = (T)NAN;
+        if (tid == 0) {
+            if (d.lse) d.lse[sh] = NAN;
+            if (d.len_out && h == 0) d.len_out[s] = n;
+        }
+        return;
+    }
+    const int t = p.plen + n;
+    const int lo = window_lo(t, d.k);
+    const FusionBias fb = fusion_bias(d.gate[s * d.gss + h * d.gsh], CLAMP);
+
+    float m = -INFINITY, l = 0.0f;
+    float acc[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) acc[e] = 0.0f;
+    // Raises the maximum to that of the row groups' logits.
+    auto raise = [&](float cmax) __attribute__((always_inline)) {
+#pragma unroll
+        for (int o = LPR; o < 64; o <<= 1) cmax = fmaxf(cmax, __shfl_xor(cmax, o));
+        const float m_new = fmaxf(m, cmax);
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) acc[e] *= alpha;
+        return m_use;
+    };
+
+    if constexpr (MODE != JOIN) {
+        const int64_t head = sh * (int64_t)d.cap;
+        uint8_t *kc = (uint8_t *)d.k_cache + (head * D + sub * EPL) * sizeof(ST);
+        uint8_t *vc = (uint8_t *)d.v_cache + (head * D + sub * EPL) * sizeof(ST);
+        constexpr int64_t RB = D * sizeof(ST);   // bytes of a row
+
+        float qf[EPL];
+        load_wide<T, EPL>((const T *)d.q_new + sh * D + sub * EPL, qf);
+        const float c2 = d.scale * kLog2e;
+
+        const int first = max(lo - p.plen, 0);   // own window rows first + [0, nwin)
+        const int nwin = n - first;
+        const int all = (nwin + RPC - 1) / RPC;
+        // this launch's chunks
+        const int per = MODE == RANGE ? (all + p.own_parts - 1) / p.own_parts : all;
+        const int chunk0 = min(range * per, all), nchunks = min(per, all - chunk0);
+
+        uint4 kr[CH], vr[CH];
+        unsigned kb[CH], vb[CH];
+        // Slots past the window read its last row again (and count as zeros below).
+        auto load = [&](int ch) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int64_t row = first + min(ch * RPC + c * RPI + rg, nwin - 1);
+                kr[c] = ONCE ? ld16_once(kc + row * RB) : ld16(kc + row * RB);
+                vr[c] = ONCE ? ld16_once(vc + row * RB) : ld16(vc + row * RB);
+                if constexpr (Q) {
+                    kb[c] = p.k_exp[head + row];
+                    vb[c] = p.v_exp[head + row];
+                }
+            }
+        };
+        // logit (log2 units) of a row from this lane's part of it
+        auto logit = [&](uint4 k, unsigned byte, float bias) __attribute__((always_inline)) {
+            float kf[EPL];
+            unpack<ST, EPL>(k, kf);
+            float part = 0.0f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) part += qf[e] * kf[e];
+            part = row_sum<LPR>(part);
+            if constexpr (Q) part *= e4m3_scale(byte);
+            if constexpr (CLAMP) return fminf(fmaxf(part * d.scale + bias, -d.clamp), d.clamp) * kLog2e;
+            return part * c2 + bias * kLog2e;
+        };
+
+        // The slot of the new row (row group 0) and the partner (row group 1),
+        // by the wavefront whose turn comes after the last chunk.
+        const bool extra = range == 0 && w == nchunks % WAVES;   // wave-uniform
+        const int jp = partner_of(t, d.k, d.pi);
+        const bool par = rg == 1 && jp >= 0;
+        uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
+        unsigned kxb = 127, vxb = 127;
+        float kn[EPL], vn[EPL];   // the new row, where it has to be quantised
+        if (extra) {
+            if (par) {
+                const bool shared = jp < p.plen;
+                const int64_t row = shared ? h * p.pcap + jp : head + (jp - p.plen);
+                const int64_t at = (row * D + sub * EPL) * (int64_t)sizeof(ST);
+                kx = ld16((shared ? (const uint8_t *)p.k_prefix : (const uint8_t *)d.k_cache) + at);
+                vx = ld16((shared ? (const uint8_t *)p.v_prefix : (const uint8_t *)d.v_cache) + at);
+                if constexpr (Q) {
+                    kxb = (shared ? p.k_prefix_exp : p.k_exp)[row];
+                    vxb = (shared ? p.v_prefix_exp : p.v_exp)[row];
+                }
+            } else if constexpr (!Q) {
+                kx = ld16((const T *)d.k_new + sh * D + sub * EPL);
+                vx = ld16((const T *)d.v_new + sh * D + sub * EPL);
+            }
+            if constexpr (Q) {
+                load_wide<T, EPL>((const T *)d.k_new + sh * D + sub * EPL, kn);
+                load_wide<T, EPL>((const T *)d.v_new + sh * D + sub * EPL, vn);
+            }
+        }
+        if (w < nchunks) load(chunk0 + w);
+        if (extra) {
+            if constexpr (Q) {
+                unsigned kby, vby;
+                const uint4 kq = quantise16<LPR>(kn, kby), vq = quantise16<LPR>(vn, vby);
+                if (!par) {
+                    kx = kq;
+                    vx = vq;
+                    kxb = kby;
+                    vxb = vby;
+                }
+            }
+            const float v = logit(kx, kxb, rg == 1 ? fb.partner : fb.local);
+            const bool entry = rg == 0 || par;
+            const float sc = entry ? v : -INFINITY;
+            m = sc;
+#pragma unroll
+            for (int o = LPR; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+            const float pr = __builtin_amdgcn_exp2f(sc - (m == -INFINITY ? 0.0f : m));
+            l = pr;
+            float vf[EPL];
+            unpack<ST, EPL>(vx, vf);
+            if (entry) {
+                const float pv = Q ? pr * e4m3_scale(vxb) : pr;
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) acc[e] = pv * vf[e];
+            }
+            // append the new row as own row n (no row read here is row n)
+            if (rg == 0) {
+                *reinterpret_cast<uint4 *>(kc + n * RB) = kx;
+                *reinterpret_cast<uint4 *>(vc + n * RB) = vx;
+                if (Q && sub == 0) {
+                    p.k_exp[head + n] = (uint8_t)kxb;
+                    p.v_exp[head + n] = (uint8_t)vxb;
+                }
+            }
+        }
+        for (int i = w; i < nchunks; i += WAVES) {
+            const int ch = chunk0 + i;
+            if (i != w) load(ch);
+            float sc[CH];
+            float cmax = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const float v = logit(kr[c], kb[c], fb.local);
+                sc[c] = ch * RPC + c * RPI + rg < nwin ? v : -INFINITY;
+                cmax = fmaxf(cmax, sc[c]);
+            }
+            const float m_use = raise(cmax);
+            if ((ch + 1) * RPC > nwin) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (ch * RPC + c * RPI + rg >= nwin) vr[c] = make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const float pr = __builtin_amdgcn_exp2f(sc[c] - m_use);
+                l += pr;
+                const float pv = Q ? pr * e4m3_scale(vb[c]) : pr;
+                float vf[EPL];
+                unpack<ST, EPL>(vr[c], vf);
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) acc[e] += pv * vf[e];
+            }
+        }
+    }
+
+    // The parts: of the prefix chunks that this window meets, and (JOIN) of the
+    // ranges of own rows.
+    if (MODE != RANGE) {
+        const int from = lo < p.plen ? max(lo - (p.plen - p.near), 0) / max(p.chunk, 1) : p.chunks;
+        const int upto = p.chunks + (MODE == JOIN ? p.own_parts : 0);
+        for (int x = from + w * RPI; x < upto; x += WAVES * RPI) {
+            const int64_t at = (int64_t)(x + rg) * n_sh + sh;
+            const bool there = x + rg < upto;
+            float2 ml = make_float2(-INFINITY, 0.0f);
+            float o[EPL];
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) o[e] = 0.0f;
+            if (there) {
+                ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                load_wide<float, EPL>(p.part_o + at * D + sub * EPL, o);
+            }
+            const float m_use = raise(ml.x);
+            const float f = __builtin_amdgcn_exp2f(ml.x - m_use);
+            l += f * ml.y;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) acc[e] += f * o[e];
+        }
+    }
+
+    // Merge the row groups of the wavefront (lanes with the same sub).
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+        l += __shfl_xor(l, o);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) acc[e] += __shfl_xor(acc[e], o);
+    }
+    if (rg == 0) {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) s_acc[w][sub * EPL + e] = acc[e];
+        if (sub == 0) {
+            s_m[w] = m;
+            s_l[w] = l;
+        }
+    }
+    __syncthreads();
+
+    for (int i = tid; i < D; i += 64 * WAVES) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) M = fmaxf(M, s_m[x]);
+        float L = 0.0f, o = 0.0f;
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) {
+            const float f = s_m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[x] - M);
+            L += s_l[x] * f;
+            o += s_acc[x][i] * f;
+        }
+        if (MODE == RANGE) {
+            const int64_t at = (int64_t)(p.chunks + range) * n_sh + sh;
+            p.part_o[at * D + i] = o;
+            if (i == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(M, L);
+        } else {
+            out[i] = (T)(o / L);
+            if (i == 0) {
+                if (d.lse) d.lse[sh] = (M + __log2f(L)) * kLn2 + fb.lse_shift;
+                if (d.len_out && h == 0) d.len_out[s] = n + 1;
+            }
+        }
+    }
+}
+
+constexpr int64_t kKeepBytes = 12 << 20;
+
+template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH>
+hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
+    const int64_t n = (int64_t)p.d.S * p.d.H;
+    const bool once = 2 * n * std::min(p.d.k, p.d.cap) * D * (int64_t)sizeof(ST) > kKeepBytes;
+    const int64_t groups = n * (MODE == RANGE ? p.own_parts : 1);
+    return launch_kernel(once ? decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, true>
+                              : decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, false>,
+                         dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
+}
+
+template <typename T, typename ST, int D, bool CLAMP>
+hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
+    const int64_t n = (int64_t)p.d.S * p.d.H;
+    const int loads = (std::min(p.d.k, p.d.cap) + Row<ST, D>::RPI - 1) / Row<ST, D>::RPI;
+    if (p.own_parts) {
+        const hipError_t e = launch_n<T, ST, D, CLAMP, RANGE, 4, 4>(p, stream);
+        return e != hipSuccess ? e : launch_n<T, ST, D, CLAMP, JOIN, 4, 4>(p, stream);
+    }
+    if (loads > 32) return launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream);
+    if (loads > 8 || (loads > 4 && n <= 1024)) return launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
+    return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
+}
+
+template <typename T, typename ST>
+hipError_t launch_t(const CachedParams &p, hipStream_t stream) {
+    const bool clamp = p.d.clamp > 0.0f;
+    if (p.d.D == 64) return clamp ? launch_w<T, ST, 64, true>(p, stream) : launch_w<T, ST, 64, false>(p, stream);
+    return clamp ? launch_w<T, ST, 128, true>(p, stream) : launch_w<T, ST, 128, false>(p, stream);
+}
+
+}  // namespace
+
+// The sizes of the parts, by the problem's sizes alone (the lengths lie in
+// device memory).
+void plan_decode_cached(CachedParams &p, bool bf16) {
+    const int64_t n = (int64_t)p.d.S * p.d.H;
+    p.near = std::min(p.d.k, p.plen);
+    p.chunk = p.chunks = p.own_parts = 0;
+    if (p.near > 0) {
+        const PrefixShape shape = prefix_shape(p.d.S, bf16);
+        const int64_t tiles = (p.near + shape.tile - 1) / shape.tile;
+        const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
+        const int64_t chunks = std::min(tiles, std::max<int64_t>(1, 512 / side));
+        const int64_t per = (tiles + chunks - 1) / chunks;
+        p.chunk = (int)(per * shape.tile);
+        p.chunks = (int)((tiles + per - 1) / per);
+    }
+    const int64_t own = std::min(p.d.k, p.d.cap - 1);
+    if (n < 256 && own >= 4096) p.own_parts = (int)std::min<int64_t>(512 / n, own / 1024);
+}
+
+hipError_t launch_decode_cached(const CachedParams &p, bool bf16, hipStream_t stream) {
+    if ((int64_t)p.d.S * p.d.H == 0) return hipSuccess;
+    if (p.chunks) {
+        const hipError_t e = launch_prefix(p, bf16, stream);
+        if (e != hipSuccess) return e;
+    }
+    if (p.k_exp) return bf16 ? launch_t<__bf16, e4m3>(p, stream) : launch_t<float, e4m3>(p, stream);
+    return bf16 ? launch_t<__bf16, __bf16>(p, stream) : launch_t<float, float>(p, stream);
+}
+
+}  // namespace pi_attn
