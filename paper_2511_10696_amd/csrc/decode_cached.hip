@@ -49,14 +49,14 @@ __device__ inline void unpack(uint4 u, float (&f)[EPL]) {
     }
 }
 
-// EPL consecutive elements of a row in the working type.
+// EPL consecutive elements of a row in the working type, from their loads.
 template <typename T, int EPL>
-__device__ inline void load_wide(const T *p, float (&f)[EPL]) {
+__device__ inline void wide_f32(const uint4 (&u)[EPL * sizeof(T) / 16], float (&f)[EPL]) {
     constexpr int N = 16 / (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < EPL / N; ++i) {
         float x[N];
-        to_f32<T>(ld16(p + i * N), x);
+        to_f32<T>(u[i], x);
 #pragma unroll
         for (int e = 0; e < N; ++e) f[i * N + e] = x[e];
     }
@@ -73,9 +73,11 @@ __device__ inline uint4 quantise16(const float (&x)[16], unsigned &byte) {
     return make_uint4(e4m3_pack4(x, inv), e4m3_pack4(x + 4, inv), e4m3_pack4(x + 8, inv), e4m3_pack4(x + 12, inv));
 }
 
-// What a launch does of a step: all of it, one range of own rows (a part), or
-// the join of the parts.
-enum { WHOLE, RANGE, JOIN };
+// What a launch does of a step: all of it, where no prefix row is in a window
+// (ALONE), where they were taken in parts (WHOLE) or are read here, by each
+// sequence for itself (DIRECT); one range of own rows (RANGE: a part), or the
+// join of the parts (JOIN).
+enum { ALONE, WHOLE, DIRECT, RANGE, JOIN };
 
 template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams p) {
@@ -97,8 +99,31 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     const int tid = threadIdx.x, lane = __lane_id();
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int sub = lane % LPR, rg = lane / LPR;
-    const int n = d.len_in[s];   // own rows
     T *out = (T *)d.out + sh * D;
+
+    // What waits for no length is on its way with it: the query, and of the parts
+    // the one that this row group joins first (of a chunk that the window does not
+    // meet it holds anything, and is left out below).
+    constexpr bool PARTS = MODE == WHOLE || MODE == JOIN;
+    constexpr int WIDE = EPL * (int)sizeof(T) / 16;   // loads of a lane's elements in the working type
+    const int n = d.len_in[s];   // own rows
+    auto load_wide = [&](const void *row, uint4 (&u)[WIDE]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < WIDE; ++i) u[i] = ld16((const T *)row + sh * D + sub * EPL + i * (EPL / WIDE));
+    };
+    uint4 qw[WIDE];
+    if constexpr (MODE != JOIN) load_wide(d.q_new, qw);
+    const int parts = PARTS ? p.chunks + (MODE == JOIN ? p.own_parts : 0) : 0;
+    float2 ml = make_float2(0.0f, 0.0f);
+    uint4 po[EPL / 4];
+    auto load_part = [&](int x) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)min(x + rg, parts - 1) * n_sh + sh;
+        ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+#pragma unroll
+        for (int i = 0; i < EPL / 4; ++i) po[i] = ld16(p.part_o + at * D + sub * EPL + 4 * i);
+    };
+    if (PARTS && w * RPI < parts) load_part(w * RPI);
+    const FusionBias fb = fusion_bias(d.gate[s * d.gss + h * d.gsh], CLAMP);
 
     if (n < 0 || n >= d.cap) {
         if (MODE == RANGE) return;
@@ -111,7 +136,6 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     }
     const int t = p.plen + n;
     const int lo = window_lo(t, d.k);
-    const FusionBias fb = fusion_bias(d.gate[s * d.gss + h * d.gsh], CLAMP);
 
     float m = -INFINITY, l = 0.0f;
     float acc[EPL];
@@ -138,11 +162,15 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
         constexpr int64_t RB = D * sizeof(ST);   // bytes of a row
 
         float qf[EPL];
-        load_wide<T, EPL>((const T *)d.q_new + sh * D + sub * EPL, qf);
+        wide_f32<T, EPL>(qw, qf);
         const float c2 = d.scale * kLog2e;
 
-        const int first = max(lo - p.plen, 0);   // own window rows first + [0, nwin)
-        const int nwin = n - first;
+        // window rows first + [0, nwin): own rows, or (DIRECT) positions
+        const int first = MODE == DIRECT ? lo : max(lo - p.plen, 0);
+        const int nwin = (MODE == DIRECT ? t : n) - first;
+        const int64_t shared = h * p.pcap;
+        const uint8_t *kp = (const uint8_t *)p.k_prefix + (shared * D + sub * EPL) * sizeof(ST);
+        const uint8_t *vp = (const uint8_t *)p.v_prefix + (shared * D + sub * EPL) * sizeof(ST);
         const int all = (nwin + RPC - 1) / RPC;
         // this launch's chunks
         const int per = MODE == RANGE ? (all + p.own_parts - 1) / p.own_parts : all;
@@ -154,12 +182,22 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
         auto load = [&](int ch) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int64_t row = first + min(ch * RPC + c * RPI + rg, nwin - 1);
-                kr[c] = ONCE ? ld16_once(kc + row * RB) : ld16(kc + row * RB);
-                vr[c] = ONCE ? ld16_once(vc + row * RB) : ld16(vc + row * RB);
+                int64_t row = first + min(ch * RPC + c * RPI + rg, nwin - 1);
+                const uint8_t *ka = kc, *va = vc;
+                const uint8_t *kea = p.k_exp + head, *vea = p.v_exp + head;
+                if constexpr (MODE == DIRECT) {
+                    const bool own = row >= p.plen;
+                    row = own ? row - p.plen : row;
+                    ka = own ? ka : kp;
+                    va = own ? va : vp;
+                    kea = own ? kea : p.k_prefix_exp + shared;
+                    vea = own ? vea : p.v_prefix_exp + shared;
+                }
+                kr[c] = ONCE ? ld16_once(ka + row * RB) : ld16(ka + row * RB);
+                vr[c] = ONCE ? ld16_once(va + row * RB) : ld16(va + row * RB);
                 if constexpr (Q) {
-                    kb[c] = p.k_exp[head + row];
-                    vb[c] = p.v_exp[head + row];
+                    kb[c] = kea[row];
+                    vb[c] = vea[row];
                 }
             }
         };
@@ -183,30 +221,27 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
         const bool par = rg == 1 && jp >= 0;
         uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
         unsigned kxb = 127, vxb = 127;
-        float kn[EPL], vn[EPL];   // the new row, where it has to be quantised
+        uint4 kw[WIDE], vw[WIDE];
         if (extra) {
-            if (par) {
-                const bool shared = jp < p.plen;
-                const int64_t row = shared ? h * p.pcap + jp : head + (jp - p.plen);
-                const int64_t at = (row * D + sub * EPL) * (int64_t)sizeof(ST);
-                kx = ld16((shared ? (const uint8_t *)p.k_prefix : (const uint8_t *)d.k_cache) + at);
-                vx = ld16((shared ? (const uint8_t *)p.v_prefix : (const uint8_t *)d.v_cache) + at);
-                if constexpr (Q) {
-                    kxb = (shared ? p.k_prefix_exp : p.k_exp)[row];
-                    vxb = (shared ? p.v_prefix_exp : p.v_exp)[row];
-                }
-            } else if constexpr (!Q) {
-                kx = ld16((const T *)d.k_new + sh * D + sub * EPL);
-                vx = ld16((const T *)d.v_new + sh * D + sub * EPL);
-            }
+            load_wide(d.k_new, kw);
+            load_wide(d.v_new, vw);
+        }
+        if (extra && par) {
+            const bool own = jp >= p.plen;
+            const int64_t row = own ? jp - p.plen : jp;
+            kx = ld16((own ? kc : kp) + row * RB);
+            vx = ld16((own ? vc : vp) + row * RB);
             if constexpr (Q) {
-                load_wide<T, EPL>((const T *)d.k_new + sh * D + sub * EPL, kn);
-                load_wide<T, EPL>((const T *)d.v_new + sh * D + sub * EPL, vn);
+                kxb = (own ? p.k_exp + head : p.k_prefix_exp + shared)[row];
+                vxb = (own ? p.v_exp + head : p.v_prefix_exp + shared)[row];
             }
         }
         if (w < nchunks) load(chunk0 + w);
         if (extra) {
             if constexpr (Q) {
+                float kn[EPL], vn[EPL];
+                wide_f32<T, EPL>(kw, kn);
+                wide_f32<T, EPL>(vw, vn);
                 unsigned kby, vby;
                 const uint4 kq = quantise16<LPR>(kn, kby), vq = quantise16<LPR>(vn, vby);
                 if (!par) {
@@ -215,6 +250,9 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
                     kxb = kby;
                     vxb = vby;
                 }
+            } else if (!par) {
+                kx = kw[0];
+                vx = vw[0];
             }
             const float v = logit(kx, kxb, rg == 1 ? fb.partner : fb.local);
             const bool entry = rg == 0 || par;
@@ -273,25 +311,19 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
 
     // The parts: of the prefix chunks that this window meets, and (JOIN) of the
     // ranges of own rows.
-    if (MODE != RANGE) {
-        const int from = lo < p.plen ? max(lo - (p.plen - p.near), 0) / max(p.chunk, 1) : p.chunks;
-        const int upto = p.chunks + (MODE == JOIN ? p.own_parts : 0);
-        for (int x = from + w * RPI; x < upto; x += WAVES * RPI) {
-            const int64_t at = (int64_t)(x + rg) * n_sh + sh;
-            const bool there = x + rg < upto;
-            float2 ml = make_float2(-INFINITY, 0.0f);
-            float o[EPL];
+    for (int x = w * RPI; x < parts; x += WAVES * RPI) {
+        if (x != w * RPI) load_part(x);
+        const int y = x + rg;
+        const bool there = y < parts && (y >= p.chunks || (lo < p.plen && lo < chunk_end(p, y)));
+        const float top = there ? ml.x : -INFINITY;
+        const float m_use = raise(top);
+        const float f = __builtin_amdgcn_exp2f(top - m_use);
+        l += there ? f * ml.y : 0.0f;
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) o[e] = 0.0f;
-            if (there) {
-                ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
-                load_wide<float, EPL>(p.part_o + at * D + sub * EPL, o);
-            }
-            const float m_use = raise(ml.x);
-            const float f = __builtin_amdgcn_exp2f(ml.x - m_use);
-            l += f * ml.y;
+        for (int i = 0; i < EPL / 4; ++i) {
+            const f32x4 o = __builtin_bit_cast(f32x4, po[i]);
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) acc[e] += f * o[e];
+            for (int e = 0; e < 4; ++e) acc[4 * i + e] += there ? f * o[e] : 0.0f;
         }
     }
 
@@ -342,7 +374,7 @@ constexpr int64_t kKeepBytes = 12 << 20;
 template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH>
 hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
-    const bool once = 2 * n * std::min(p.d.k, p.d.cap) * D * (int64_t)sizeof(ST) > kKeepBytes;
+    const bool once = MODE != DIRECT && 2 * n * std::min(p.d.k, p.d.cap) * D * (int64_t)sizeof(ST) > kKeepBytes;
     const int64_t groups = n * (MODE == RANGE ? p.own_parts : 1);
     return launch_kernel(once ? decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, true>
                               : decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, false>,
@@ -352,14 +384,24 @@ hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
 template <typename T, typename ST, int D, bool CLAMP>
 hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
-    const int loads = (std::min(p.d.k, p.d.cap) + Row<ST, D>::RPI - 1) / Row<ST, D>::RPI;
+    const int rows = std::min(p.d.k, p.d.cap) + (p.direct ? p.near : 0);
+    const int loads = (rows + Row<ST, D>::RPI - 1) / Row<ST, D>::RPI;
+    if (p.direct) {
+        if (loads > 32) return launch_n<T, ST, D, CLAMP, DIRECT, 8, 4>(p, stream);
+        return launch_n<T, ST, D, CLAMP, DIRECT, 4, 4>(p, stream);
+    }
     if (p.own_parts) {
         const hipError_t e = launch_n<T, ST, D, CLAMP, RANGE, 4, 4>(p, stream);
         return e != hipSuccess ? e : launch_n<T, ST, D, CLAMP, JOIN, 4, 4>(p, stream);
     }
-    if (loads > 32) return launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream);
-    if (loads > 8 || (loads > 4 && n <= 1024)) return launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
-    return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
+    if (p.chunks) {
+        if (loads > 32) return launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream);
+        if (loads > 8) return launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
+        return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
+    }
+    if (loads > 32) return launch_n<T, ST, D, CLAMP, ALONE, 8, 4>(p, stream);
+    if (loads > 8 || (loads > 4 && n <= 1024)) return launch_n<T, ST, D, CLAMP, ALONE, 4, 4>(p, stream);
+    return launch_n<T, ST, D, CLAMP, ALONE, 2, 2>(p, stream);
 }
 
 template <typename T, typename ST>
@@ -371,28 +413,43 @@ hipError_t launch_t(const CachedParams &p, hipStream_t stream) {
 
 }  // namespace
 
+#ifndef DIRECT_EL
+#define DIRECT_EL (4 << 20)
+#endif
+constexpr int64_t kDirectElements = DIRECT_EL;
+
+// At most `most` chunks of whole tiles, as even as they can be.
+int64_t even_chunks(const CachedParams &p, int64_t most) {
+    const int64_t tiles = (p.near + p.tile - 1) / p.tile, per = (tiles + most - 1) / most;
+    return (tiles + per - 1) / per;
+}
+
 // The sizes of the parts, by the problem's sizes alone (the lengths lie in
 // device memory).
 void plan_decode_cached(CachedParams &p, bool bf16) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
     p.near = std::min(p.d.k, p.plen);
-    p.chunk = p.chunks = p.own_parts = 0;
-    if (p.near > 0) {
-        const PrefixShape shape = prefix_shape(p.d.S, bf16);
-        const int64_t tiles = (p.near + shape.tile - 1) / shape.tile;
-        const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
-        const int64_t chunks = std::min(tiles, std::max<int64_t>(1, 512 / side));
-        const int64_t per = (tiles + chunks - 1) / chunks;
-        p.chunk = (int)(per * shape.tile);
-        p.chunks = (int)((tiles + per - 1) / per);
-    }
+    p.tile = p.chunks = p.own_parts = 0;
     const int64_t own = std::min(p.d.k, p.d.cap - 1);
+    p.direct = p.near > 0 && n * (p.near + own) * p.d.D <= kDirectElements;
+    if (p.near > 0 && !p.direct) {
+        // the most chunks that any caches' type takes
+        const PrefixShape shape = prefix_shape(p, bf16);
+        p.tile = !bf16 && p.d.S <= 32 ? 64 : 128;
+        const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
+        p.chunks = (int)even_chunks(p, std::max<int64_t>(1, 512 / side));
+    }
     if (n < 256 && own >= 4096) p.own_parts = (int)std::min<int64_t>(512 / n, own / 1024);
 }
 
-hipError_t launch_decode_cached(const CachedParams &p, bool bf16, hipStream_t stream) {
+hipError_t launch_decode_cached(const CachedParams &planned, bool bf16, hipStream_t stream) {
+    CachedParams p = planned;
     if ((int64_t)p.d.S * p.d.H == 0) return hipSuccess;
     if (p.chunks) {
+        const PrefixShape shape = prefix_shape(p, bf16);
+        const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
+        p.tile = shape.tile;
+        p.chunks = (int)even_chunks(p, std::min<int64_t>(p.chunks, std::max<int64_t>(1, 256 * shape.per_cu / side)));
         const hipError_t e = launch_prefix(p, bf16, stream);
         if (e != hipSuccess) return e;
     }

@@ -92,9 +92,16 @@ struct CachedParams {
     // at[x][s * H + h] the weighted values [D], then (max, sum) in log2 units.
     float *part_o, *part_ml;
     int near;                       // prefix rows from which on windows reach: [plen - near, plen)
-    int chunk, chunks;              // rows of a chunk of them, chunks
+    int tile, chunks;               // their tiles' rows; chunk x takes tiles x, x + chunks, ...
     int own_parts;
+    bool direct;                    // prefix rows are read with the own ones, no chunks
 };
+
+// Behind the last row of a chunk: it is of no use to windows that begin there or later.
+__host__ __device__ inline int chunk_end(const CachedParams &p, int x) {
+    const int tiles = (p.near + p.tile - 1) / p.tile, last = x + (tiles - 1 - x) / p.chunks * p.chunks;
+    return last + 1 == tiles ? p.plen : p.plen - p.near + (last + 1) * p.tile;
+}
 
 struct BwdParams {
     FwdParams f;                    // inputs as for the forward (out/lse unused)
@@ -127,9 +134,10 @@ hipError_t launch_decode_cached(const CachedParams &p, bool bf16, hipStream_t st
 // Its shared prefix: the parts of the chunks.
 struct PrefixShape {
     int queries;                    // of a work-group
-    int tile;                       // rows of a tile: a chunk is whole tiles
+    int tile;                       // rows that it takes at a time, 128 at most (float32: of <= 16 sequences 64)
+    int per_cu;                     // work-groups that share a CU
 };
-PrefixShape prefix_shape(int S, bool bf16);
+PrefixShape prefix_shape(const CachedParams &p, bool bf16);
 hipError_t launch_prefix(const CachedParams &p, bool bf16, hipStream_t stream);
 
 // Rows into (store) or out of a quantised cache.

@@ -9,24 +9,31 @@
 // logit m of the chunk (log2 units), l = sum 2^(x - m) and the values weighted
 // alike, o; decode_cached.hip joins the chunks with the sequence's own rows.
 //
-// Tiles of rows go through LDS in the working type: the loads of the next tile
-// (16 bytes a thread, whole lines) are issued before the present one is worked
-// on and written behind it, e4m3 codes converted on the way, with the row's
-// scale, which is exact.  The four wavefronts of a work-group are G groups of
-// queries by RS shares of a tile's row blocks; with few sequences all four
-// share one group of queries, and their states are joined at the end.
+// Rows go from global memory straight into LDS as they are stored, through a
+// ring of stages: while a stage is worked on, the next ones are on their way,
+// and a wait counts the loads that may stay in flight.  The 16-byte pieces of a
+// row are XOR-swizzled by the row, each lane fetching the piece that belongs at
+// its place, so that no operand read below meets a bank twice.  e4m3 codes are
+// converted as they become operands: a key row's scale with its codes (exact),
+// a value row's in the weight (exact).  The four wavefronts of a work-group are
+// G groups of queries by RS shares of a stage's row blocks.  With one group
+// every wavefront has a ring of its own, and they wait for nobody until their
+// states are joined at the end.
 //
 // As in forward_bf16.hip the scores are computed transposed, S^T = K Q^T, so
 // that a lane holds scores of one query and the probabilities are the B operand
 // of O^T = V^T P^T as they lie, the row order permuted alike in the V^T operand
-// (bf16: LDS transpose reads).  The running maximum is raised with every block
-// that has a larger logit, so a dominating row has weight 1 before it is
-// rounded to bf16; the sums are of the unrounded weights.
+// (LDS transpose reads).  The running maximum is raised with every block that
+// has a larger logit, so a dominating row has weight 1 before it is rounded to
+// bf16; the sums are of the unrounded weights.
 //
 // Rows that begin before a sequence's window are masked in the blocks that
 // hold such rows.  A masked weight is 0, but 0 times an infinity or NaN is not:
-// tiles with masked rows are searched for values that are not finite, and one
-// that has some is added entry by entry.
+// blocks with masked rows are searched for values that are not finite; these
+// become 0 in LDS, and where there were any, they are added at the end, row by
+// row, for the sequences that do attend them.  (Added in their block, by
+// instructions other than the product's, they cost the product's loop 80
+// registers.)
 #include <algorithm>
 
 #include "bf16_rows.h"
@@ -39,264 +46,496 @@ namespace pi_attn {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
-constexpr int WAVES = 4;
-constexpr int NT = 64 * WAVES;
+// ---- rows as they lie in LDS -----------------------------------------------------
+// Row r of a block: piece pc (16 bytes) at place pc ^ key(r) of the keys' and pc ^
+// value(r) of the values'.
+template <typename ST, int D>
+struct Rows {
+    static constexpr int RB = D * (int)sizeof(ST);   // bytes
+    static constexpr int CPR = RB / 16;              // pieces
+    // The keys' reads: 16 lanes, 16 rows, one piece each.
+    static __device__ int key(int r) { return (RB >= 256 ? r : r / (256 / RB)) & (CPR < 16 ? CPR - 1 : 15); }
+    // The values': 4 rows of 64 bytes (bf16), 8 rows of 32 bytes (e4m3, rows r..r+3 and r+8..r+11), rows r, r + 4, r + 8,
+    // r + 12 of 64 bytes (float32).
+    static __device__ int value(int r) {
+        if constexpr (sizeof(ST) == 4) return 4 * ((r >> 2) & 3);
+        if constexpr (sizeof(ST) == 2) return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1);
+        return D == 128 ? 2 * ((r >> 1) & 1) + 4 * ((r >> 3) & 1) : 2 * ((r >> 3) & 1);
+    }
+    // The bits of a word's elements that are not finite: all ones for each of them.
+    static __device__ unsigned not_finite(unsigned w) {
+        if constexpr (sizeof(ST) == 4) return (w & 0x7f800000u) == 0x7f800000u ? ~0u : 0u;
+        unsigned high;   // the top bit of each such element
+        if constexpr (sizeof(ST) == 2) high = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        if constexpr (sizeof(ST) == 1) high = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // codes 0x7f, 0xff
+        constexpr int N = sizeof(ST) == 2 ? 16 : 8;
+        return (high >> (N - 1)) * (unsigned)((1ull << N) - 1);
+    }
+};
 
-// ---- one block of rows with one group of queries ------------------------------
-// Lane (c, g) belongs to query c of the group.  QB queries and KB rows a block;
-// NS score slots, slot i being row slot_row(i, g); the output's groups of four
-// dims, group x being dims ODIM * x + 4 g + [0, 4).
-template <typename T, int D>
+__device__ inline float element(float x) { return x; }
+__device__ inline float element(__bf16 x) { return (float)x; }
+__device__ inline float element(e4m3 x) { return __builtin_amdgcn_cvt_f32_fp8((int)x.code, 0); }
+
+__device__ inline uint4 lds16(const unsigned char *p) { return *reinterpret_cast<const uint4 *>(p); }
+
+// Eight bf16 values of eight codes, times scale.
+__device__ inline bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// ---- one block of rows with a wavefront's queries -------------------------------
+// NG groups of QB queries, which share the operands made of the rows; lane (c, g)
+// belongs to query c of each.  KB rows a block; NS score slots, slot i being row
+// slot_row(i, g) (four slots in a row are four rows in a row); the output's NO
+// groups of four dims, group x being dims ODIM * x + 4 g + [0, 4).
+template <typename T, typename ST, int D, int NG>
 struct Mma;
 
-template <int D>
-struct Mma<__bf16, D> {
+template <typename ST, int D, int NG>
+struct Mma<__bf16, ST, D, NG> {
+    using R = Rows<ST, D>;
+    static constexpr bool Q = sizeof(ST) == 1;
     static constexpr int QB = 32, KB = 32, NS = 16, NO = D / 8, ODIM = 8;
-    static constexpr int KROW = 2 * D + 16, VROW = 2 * D + 64;   // bytes of a row in LDS: no bank met twice
-    bf16x8 qf[D / 16];
-    f32x16 o[D / 32];
+    bf16x8 qf[NG][D / 16];
+    f32x16 o[NG][D / 32];
 
     static __device__ int slot_row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
-    __device__ void query(const __bf16 *q, int g) {
+    // Product step s contracts dims dim0(s, g) + [0, 8).
+    static __device__ int dim0(int s, int g) { return Q ? 32 * (s >> 1) + 16 * g + 8 * (s & 1) : 16 * s + 8 * g; }
+    __device__ void query(int n, const __bf16 *q, int g, bool there) {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[s] = *reinterpret_cast<const bf16x8 *>(q + 16 * s + 8 * g);
+        for (int s = 0; s < D / 16; ++s)
+            qf[n][s] = there ? *reinterpret_cast<const bf16x8 *>(q + dim0(s, g)) : bf16x8{};
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) o[n][b] = f32x16{};
     }
-    __device__ void clear() {
+    __device__ void query_landed() {
 #pragma unroll
-        for (int b = 0; b < D / 32; ++b) o[b] = f32x16{};
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                u32x4 u = __builtin_bit_cast(u32x4, qf[n][s]);
+                asm volatile("" : "+v"(u));
+                qf[n][s] = __builtin_bit_cast(bf16x8, u);
+            }
     }
-    __device__ void clear_query() {
+    __device__ void scale(int n, float a) {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[s] = bf16x8{};
+        for (int b = 0; b < D / 32; ++b) o[n][b] *= a;
     }
-    __device__ void scale(float a) {
+    __device__ float &at(int n, int x, int e) { return reinterpret_cast<float *>(&o[n][x >> 2])[4 * (x & 3) + e]; }
+    // A block's operands as they lie in LDS.
+    uint4 kr[R::CPR / 2];
+    uint2 vr[2][D / 32][Q ? 1 : 2];
+    __device__ void read_keys(const unsigned char *kt, int c, int g) {
+        const unsigned char *row = kt + c * R::RB;
+        const int sw = R::key(c);
 #pragma unroll
-        for (int b = 0; b < D / 32; ++b) o[b] *= a;
+        for (int u = 0; u < R::CPR / 2; ++u) kr[u] = lds16(row + ((2 * u + g) ^ sw) * 16);
     }
-    __device__ float &at(int x, int e) { return reinterpret_cast<float *>(&o[x >> 2])[4 * (x & 3) + e]; }
-    __device__ void scores(const unsigned char *kt, int c, int g, float (&s)[NS]) const {
-        bf16x8 kf[D / 16];
+    __device__ void read_values(const unsigned char *vt, int lane) {
+        const int g = lane >> 5, half = (lane >> 4) & 1;
+        if constexpr (Q) {
+            // the 16 lanes of a half: eight rows (two lanes each) by 16 dims
+            const int i = lane & 15, pr = i >> 1, row = 8 * (pr >> 2) + 4 * g + (pr & 3);
+            const unsigned char *at = vt + row * R::RB + (i & 1) * 8;
+            const int sw = R::value(row);
 #pragma unroll
-        for (int u = 0; u < D / 16; ++u) kf[u] = *reinterpret_cast<const bf16x8 *>(kt + c * KROW + (2 * u + g) * 16);
-        f32x16 sc = {};
+            for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-        for (int u = 0; u < D / 16; ++u) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u], qf[u], sc, 0, 0, 0);
+                for (int b = 0; b < D / 32; ++b)
+                    vr[cc][b][0] = __builtin_bit_cast(
+                        uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                   (lds_i32x2 *)(at + 16 * cc * R::RB + ((2 * b + half) ^ sw) * 16)));
+        } else {
+            const int r = (lane >> 2) & 3, qd = lane & 3;
+            const unsigned char *at = vt + (4 * g + r) * R::RB + (qd & 1) * 8;
+            const int sw = R::value(r);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) s[i] = sc[i];
+            for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh)
+                        vr[cc][b][hh] = __builtin_bit_cast(
+                            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (lds_s16x4 *)(at + (16 * cc + 8 * hh) * R::RB +
+                                                     ((4 * b + 2 * half + (qd >> 1)) ^ sw) * 16)));
+        }
     }
-    __device__ void values(const unsigned char *vt, int lane, const float (&p)[NS]) {
-        const int g = lane >> 5, G = lane >> 4, r = (lane >> 2) & 3, qd = lane & 3;
+    __device__ void scores(float kscale, float (&s)[NG][NS]) const {
+        f32x16 sc[NG] = {};
+#pragma unroll
+        for (int u = 0; u < D / 16; ++u) {
+            bf16x8 kf;
+            if constexpr (Q) {
+                const uint4 k = kr[u >> 1];
+                kf = u & 1 ? widen8(k.z, k.w, kscale) : widen8(k.x, k.y, kscale);
+            } else {
+                kf = __builtin_bit_cast(bf16x8, kr[u]);
+            }
+#pragma unroll
+            for (int n = 0; n < NG; ++n) sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[n][u], sc[n], 0, 0, 0);
+        }
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) s[n][i] = sc[n][i];
+    }
+    __device__ void values(const float (&p)[NG][NS]) {
 #pragma unroll
         for (int cc = 0; cc < 2; ++cc) {
-            bf16x8 pb;
+            bf16x8 pb[NG];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pb[e] = (__bf16)p[8 * cc + e];
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pb[n][e] = (__bf16)p[n][8 * cc + e];
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) {
                 bf16x8 vf;
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int row = 16 * cc + 8 * hh + 4 * g + r, chunk = 4 * b + 2 * (G & 1) + (qd >> 1);
-                    const bf16x4 y = __builtin_bit_cast(
-                        bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (lds_s16x4 *)(vt + row * VROW + chunk * 16 + (qd & 1) * 8)));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) vf[4 * hh + e] = y[e];
+                if constexpr (Q) {
+                    vf = widen8(vr[cc][b][0].x, vr[cc][b][0].y, 1.0f);
+                } else {
+                    const uint2 lo = vr[cc][b][0], hi = vr[cc][b][1];
+                    vf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[b], 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+                    o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[n], o[n][b], 0, 0, 0);
             }
         }
     }
-    static __device__ float round(float p) { return (float)(__bf16)p; }
+    // This lane's part of its query's product with a row (without a scale).
+    __device__ float dot(int n, const ST *k, int g) const {
+        float x = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x = __builtin_fmaf((float)qf[n][s][e], element(k[dim0(s, g) + e]), x);
+        return x;
+    }
 };
 
-template <int D>
-struct Mma<float, D> {
+template <typename ST, int D, int NG>
+struct Mma<float, ST, D, NG> {
+    using R = Rows<ST, D>;
+    static constexpr bool Q = sizeof(ST) == 1;
     static constexpr int QB = 16, KB = 16, NS = 4, NO = D / 16, ODIM = 16;
-    static constexpr int KROW = 4 * D + 16, VROW = 4 * D + 16;
-    f32x4 qf[D / 16];
-    f32x4 o[D / 16];
+    f32x4 qf[NG][D / 16];
+    f32x4 o[NG][D / 16];
 
     static __device__ int slot_row(int i, int g) { return 4 * g + i; }
-    __device__ void query(const float *q, int g) {
+    // Product steps (s, e) contract dims dim0(s, g) + e.
+    static __device__ int dim0(int s, int g) { return Q ? 64 * (s >> 2) + 16 * g + 4 * (s & 3) : 16 * s + 4 * g; }
+    __device__ void query(int n, const float *q, int g, bool there) {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[s] = *reinterpret_cast<const f32x4 *>(q + 16 * s + 4 * g);
-    }
-    __device__ void clear() {
+        for (int s = 0; s < D / 16; ++s) qf[n][s] = there ? *reinterpret_cast<const f32x4 *>(q + dim0(s, g)) : f32x4{};
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) o[b] = f32x4{};
+        for (int b = 0; b < D / 16; ++b) o[n][b] = f32x4{};
     }
-    __device__ void clear_query() {
+    __device__ void query_landed() {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[s] = f32x4{};
-    }
-    __device__ void scale(float a) {
+        for (int n = 0; n < NG; ++n)
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) o[b] *= a;
+            for (int s = 0; s < D / 16; ++s) asm volatile("" : "+v"(qf[n][s]));
     }
-    __device__ float &at(int x, int e) { return reinterpret_cast<float *>(&o[x])[e]; }
-    // Product step (u, e) contracts dims 16 u + 4 g + e, in four chains.
-    __device__ void scores(const unsigned char *kt, int c, int g, float (&s)[NS]) const {
-        f32x4 sc[4] = {};
+    __device__ void scale(int n, float a) {
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) o[n][b] *= a;
+    }
+    __device__ float &at(int n, int x, int e) { return reinterpret_cast<float *>(&o[n][x])[e]; }
+    // A block's operands as they lie in LDS.
+    uint4 kr[R::CPR / 4];
+    unsigned vr[D / 16][Q ? 1 : NS];   // e4m3: four rows of dim 16 b + c
+    __device__ void read_keys(const unsigned char *kt, int c, int g) {
+        const unsigned char *row = kt + c * R::RB;
+        const int sw = R::key(c);
+#pragma unroll
+        for (int u = 0; u < R::CPR / 4; ++u) kr[u] = lds16(row + ((4 * u + g) ^ sw) * 16);
+    }
+    __device__ void read_values(const unsigned char *vt, int lane) {
+        const int c = lane & 15, g = lane >> 4;
+        if constexpr (Q) {
+            // four rows (two lanes each) of 16 dims, then the same rows of the next 16
+            const int pr = c >> 1, row = 4 * g + (pr & 3);
+            const unsigned char *at = vt + row * R::RB + (c & 1) * 8;
+            const int sw = R::value(row);
+#pragma unroll
+            for (int b = 0; b < D / 16; b += 2) {
+                const i32x2 y =
+                    __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(at + ((b + (pr >> 2)) ^ sw) * 16));
+                vr[b][0] = (unsigned)y.x;
+                vr[b + 1][0] = (unsigned)y.y;
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    const int row = 4 * g + i;
+                    vr[b][i] = *reinterpret_cast<const unsigned *>(
+                        vt + row * R::RB + ((4 * b + (c >> 2)) ^ R::value(row)) * 16 + (c & 3) * 4);
+                }
+        }
+    }
+    // In four chains.
+    __device__ void scores(float kscale, float (&s)[NG][NS]) const {
+        f32x4 sc[NG][4] = {};
 #pragma unroll
         for (int u = 0; u < D / 16; ++u) {
-            const f32x4 kf = *reinterpret_cast<const f32x4 *>(kt + c * KROW + (4 * u + g) * 16);
+            float kf[4];
+            if constexpr (Q) {
+                const uint4 k = kr[u >> 2];
+                const unsigned w[4] = {k.x, k.y, k.z, k.w};
+                e4m3_unpack4(w[u & 3], kf);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[u][e], sc[e], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) kf[e] *= kscale;
+            } else {
+                const f32x4 k = __builtin_bit_cast(f32x4, kr[u]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kf[e] = k[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+                    sc[n][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[n][u][e], sc[n][e], 0, 0, 0);
         }
-        const f32x4 sum = (sc[0] + sc[1]) + (sc[2] + sc[3]);
 #pragma unroll
-        for (int i = 0; i < NS; ++i) s[i] = sum[i];
+        for (int n = 0; n < NG; ++n) {
+            const f32x4 sum = (sc[n][0] + sc[n][1]) + (sc[n][2] + sc[n][3]);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) s[n][i] = sum[i];
+        }
     }
     // Step i contracts rows 4 g + i, whose weights are the score slots i.
-    __device__ void values(const unsigned char *vt, int lane, const float (&p)[NS]) {
-        const int c = lane & 15, g = lane >> 4;
+    __device__ void values(const float (&p)[NG][NS]) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
+        for (int b = 0; b < D / 16; ++b) {
+            float vf[NS];
+            if constexpr (Q) {
+                e4m3_unpack4(vr[b][0], vf);
+            } else {
 #pragma unroll
-            for (int b = 0; b < D / 16; ++b) {
-                const float v = *reinterpret_cast<const float *>(vt + (4 * g + i) * VROW + (16 * b + c) * 4);
-                o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i], o[b], 0, 0, 0);
+                for (int i = 0; i < NS; ++i) vf[i] = __uint_as_float(vr[b][i]);
             }
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+                    o[n][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i], p[n][i], o[n][b], 0, 0, 0);
+        }
     }
-    static __device__ float round(float p) { return p; }
+    __device__ float dot(int n, const ST *k, int g) const {
+        float x = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x = __builtin_fmaf(qf[n][s][e], element(k[dim0(s, g) + e]), x);
+        return x;
+    }
 };
 
 // Maximum and sum over the lanes of a query.
+__device__ inline float other_row(float x) {   // of the neighbouring 16 lanes
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(__lane_id() & 16 ? p[0] : p[1]);
+}
+
+// Smallest and largest of the wavefront's whole numbers: round the 16 lanes of a
+// row, then across rows.
+template <bool MAX>
+__device__ inline int wave_extreme(int x) {
+    auto join = [](int a, int b) { return MAX ? max(a, b) : min(a, b); };
+    x = join(x, __builtin_amdgcn_mov_dpp(x, 0x128, 0xF, 0xF, false));
+    x = join(x, __builtin_amdgcn_mov_dpp(x, 0x124, 0xF, 0xF, false));
+    x = join(x, __builtin_amdgcn_mov_dpp(x, 0x122, 0xF, 0xF, false));
+    x = join(x, __builtin_amdgcn_mov_dpp(x, 0x121, 0xF, 0xF, false));
+    x = join(x, __float_as_int(other_row(__int_as_float(x))));
+    x = join(x, __float_as_int(other_half(__int_as_float(x))));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
 template <int QB>
 __device__ inline float query_max(float x) {
-    if constexpr (QB == 16) x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    if constexpr (QB == 16) x = fmaxf(x, other_row(x));
+    return fmaxf(x, other_half(x));
 }
 
 template <int QB>
 __device__ inline float query_sum(float x) {
-    if constexpr (QB == 16) x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    if constexpr (QB == 16) x += other_row(x);
+    return x + other_half(x);
 }
 
-// ---- tiles ---------------------------------------------------------------------
-template <typename T, typename ST, int D, int TR>
-struct Stage {
-    using M = Mma<T, D>;
+// ---- the ring ----------------------------------------------------------------------
+// G wavefronts side by side over the queries (NG groups each), RS shares of a
+// stage's blocks.  OWN: a ring for each wavefront, whose stages are one block;
+// else one for all, of SR rows a stage.
+//
+// Two work-groups of four wavefronts share a CU where two stages of each fit.
+// float32 work-groups of one ring have eight and a CU each.
+template <typename T, typename ST, int D, int G, int NG>
+struct Shape {
+    using Type = T;
+    using M = Mma<T, ST, D, NG>;
+    using R = Rows<ST, D>;
+    using Stored = ST;
+    static constexpr int DIM = D;
     static constexpr bool Q = sizeof(ST) == 1;
-    static constexpr int CPR = D * (int)sizeof(ST) / 16;   // 16-byte pieces of a row as it is stored
-    static constexpr int U = TR * CPR / NT;                // of each thread, of keys and of values
-    static_assert(TR * CPR % NT == 0, "whole pieces for every thread");
-    uint4 k[U], v[U];
-    unsigned kb[Q ? U : 1], vb[Q ? U : 1];
-
-    // Tile rows row0 + [0, TR) of the head's rows; from `end` on row end - 1
-    // again, written as zeros by put().
-    __device__ void fetch(const CachedParams &p, int h, int row0, int end, int tid) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int x = u * NT + tid;
-            const int64_t row = h * p.pcap + min(row0 + x / CPR, end - 1);
-            const int64_t at = row * (D * (int)sizeof(ST)) + (x % CPR) * 16;
-            k[u] = *reinterpret_cast<const uint4 *>((const uint8_t *)p.k_prefix + at);
-            v[u] = *reinterpret_cast<const uint4 *>((const uint8_t *)p.v_prefix + at);
-            if constexpr (Q) {
-                kb[u] = p.k_prefix_exp[row];
-                vb[u] = p.v_prefix_exp[row];
-            }
-        }
-    }
-
-    // A piece into LDS, and whether one of its values is not finite.
-    static __device__ bool put_piece(uint4 raw, unsigned byte, unsigned char *to) {
-        unsigned bad = 0;
-        if constexpr (Q) {
-            const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
-            const float scale = e4m3_scale(byte);
-            if constexpr (sizeof(T) == 2) {
-                bf16x8 y[2];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false);
-                    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true);
-                    y[i >> 1][4 * (i & 1)] = a[0];
-                    y[i >> 1][4 * (i & 1) + 1] = a[1];
-                    y[i >> 1][4 * (i & 1) + 2] = b[0];
-                    y[i >> 1][4 * (i & 1) + 3] = b[1];
-                }
-                reinterpret_cast<bf16x8 *>(to)[0] = y[0];
-                reinterpret_cast<bf16x8 *>(to)[1] = y[1];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4 y;
-                    float x[4];
-                    e4m3_unpack4(w[i], x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = x[e] * scale;
-                    reinterpret_cast<f32x4 *>(to)[i] = y;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bad |= ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x7f, 0xff
-            bad |= byte >= 247;   // 256 * 2^120 is past the largest float
-        } else {
-            *reinterpret_cast<uint4 *>(to) = raw;
-            const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 2) {   // exponents of all ones
-                    bad |= ((w[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                } else {
-                    bad |= ((w[i] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
-                }
-            }
-        }
-        return bad != 0;
-    }
-
-    // The fetched tile into LDS; whether a value is not finite.
-    __device__ bool put(unsigned char *kt, unsigned char *vt, int row0, int end, int tid) {
-        bool bad = false;
-        constexpr int WIDE = 16 * (int)(sizeof(T) / sizeof(ST));   // bytes of a piece in LDS
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int x = u * NT + tid, r = x / CPR, pc = x % CPR;
-            if (row0 + r >= end) k[u] = v[u] = make_uint4(0, 0, 0, 0);
-            put_piece(k[u], Q ? kb[u] : 0, kt + r * M::KROW + pc * WIDE);
-            bad |= put_piece(v[u], Q ? vb[u] : 0, vt + r * M::VROW + pc * WIDE);
-        }
-        return bad;
-    }
+    static constexpr bool OWN = G == 1;
+    static constexpr int WAVES = OWN || sizeof(T) == 2 ? 4 : 8, NT = 64 * WAVES;
+    static constexpr int RS = WAVES / G;
+    static constexpr int SIDE = G, GROUPS = NG;
+    static constexpr int QT = M::QB * NG * G;                                     // queries of a work-group
+    static constexpr bool SMALL = M::KB * RS <= 64 && R::CPR >= WAVES;            // whole loads of 64 rows
+    static constexpr int SR = OWN ? M::KB : SMALL ? 64 : 128;                     // rows of a stage
+    static constexpr int TR = OWN ? WAVES * M::KB : SR;                           // rows that a work-group takes at a time
+    static constexpr int BL = OWN ? 1 : SR / M::KB / RS;                          // blocks of a wavefront among them
+    static constexpr int TABLE = SR * R::RB;                                      // bytes of the stage's keys
+    static constexpr int STAGE = 2 * TABLE + (Q ? 8 * SR : 0);                    // and values, scale bytes (a word each)
+    static constexpr int RINGS = OWN ? WAVES : 1;
+    static constexpr bool TWO = WAVES == 4 && 2 * RINGS * STAGE <= 80 << 10 && !(D == 128 && NG == 2);
+    // as many stages as fit, two at least and four at most
+    static constexpr int FIT = (TWO ? 80 << 10 : 156 << 10) / (RINGS * STAGE);
+    static constexpr int NST = FIT > 4 ? 4 : FIT;
+    static constexpr int KI = SR * R::CPR / 64 / (OWN ? 1 : WAVES);   // a wavefront's loads of a stage's keys
+    static constexpr int LOADS = 2 * KI + (Q ? (OWN ? 2 : 1) : 0);    // and of everything
+    static constexpr int PITCH = D + 4;                               // floats from one query's o to the next
+    static constexpr int RING_BYTES = RINGS * NST * STAGE;
+    static constexpr int JOIN_BYTES = WAVES * M::QB * (PITCH * 4 + 16);   // the wavefronts' states of a group
+    static constexpr int LDS = RING_BYTES > JOIN_BYTES ? RING_BYTES : JOIN_BYTES;
+    static_assert(SR * R::CPR % (64 * (OWN ? 1 : WAVES)) == 0 && BL >= 1 && NST >= 2, "whole loads, whole blocks");
 };
 
-// G groups of queries, RS = 4 / G shares of the blocks of a tile of TR rows.
-template <typename T, typename ST, int D, int G, int TR>
-__global__ __launch_bounds__(NT, TR * D > 64 * 128 ? 1 : 2) void prefix_kernel(CachedParams p, int n_qt, uint32_t n_logical) {
-    using M = Mma<T, D>;
-    constexpr int RS = WAVES / G, QB = M::QB, KB = M::KB, QT = QB * G;
-    constexpr int TILE_BYTES = TR * (M::KROW + M::VROW);
-    constexpr int STATE = 64 * 4 * (M::NO * 4 + 2);   // of a wavefront: o, m, l
-    constexpr int LDS = TILE_BYTES > (RS - 1) * G * STATE ? TILE_BYTES : (RS - 1) * G * STATE;
-    __shared__ __align__(16) unsigned char lds[LDS];
-    __shared__ int s_bad[2];
-    unsigned char *const kt = lds, *const vt = lds + TR * M::KROW;
+// lds_fetch16 of rows that are not to be kept in the caches.
+__device__ inline void lds_fetch16_once(u32x4 rsrc, int voff, void *lds) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(
+        (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
+}
+
+// One byte a lane into the words at lds + 4 * lane.
+__device__ inline void lds_fetch1(u32x4 rsrc, int voff, void *lds) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(
+        (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+    asm volatile("buffer_load_ubyte %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
+}
+
+// Waits until at most N of this wavefront's loads are on their way.
+template <int N>
+__device__ inline void wait_loads() {
+    static_assert(N < 64, "a six-bit counter");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// ONCE: the prefix's rows are not kept in the caches.
+template <typename S, bool ONCE>
+__global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void prefix_kernel(CachedParams p, int n_qt,
+                                                                                  uint32_t n_logical) {
+    using T = typename S::Type;
+    using ST = typename S::Stored;
+    using M = typename S::M;
+    using R = typename S::R;
+    constexpr bool Q = S::Q;
+    constexpr int D = S::DIM, G = S::SIDE, NG = S::GROUPS, WAVES = S::WAVES, NT = S::NT;
+    constexpr int RS = S::RS, QB = M::QB, KB = M::KB, QT = S::QT, NST = S::NST;
+    __shared__ __align__(16) unsigned char lds[S::LDS];
+    __shared__ int s_cleaned;   // !OWN: some wavefront has
 
     const uint32_t logical = xcd_remap(blockIdx.x, n_logical);
     if (logical >= n_logical) return;
     const DecodeParams &d = p.d;
     const DivMod qt_of = divmod(logical, n_qt), chunk_of = divmod(qt_of.quot, p.chunks);
     const int qt = (int)qt_of.rem, x = (int)chunk_of.rem, h = (int)chunk_of.quot;
-    const int row_begin = p.plen - p.near + x * p.chunk;
-    const int end = min(row_begin + p.chunk, p.plen);
+    // The chunk's tiles x, x + chunks, ..., the last one first: every window that
+    // meets the prefix ends with it, so the first loads wait for no length.
+    const int plen = p.plen, reach = chunk_end(p, x), step = p.chunks * S::TR;
+    const int all = (p.near - 1) / S::TR + 1;   // of all chunks
+    const int last = x + (all - 1 - x) / p.chunks * p.chunks, mine = last / p.chunks + 1;   // and of this one
+    const int row_last = plen - p.near + last * S::TR;
 
     const int tid = threadIdx.x, lane = __lane_id();
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int qg = w % G, rs = w / G;
     const int c = lane % QB, g = lane / QB;
 
+    // This lane's pieces of a stage: byte offsets from the stage's first row.
+    unsigned char *const ring = lds + (S::OWN ? w * NST * S::STAGE : 0);
+    int koff[S::KI], voff[S::KI];
+#pragma unroll
+    for (int u = 0; u < S::KI; ++u) {
+        const int y = 64 * (S::OWN ? u : u * WAVES + w) + lane, r = y / R::CPR, pc = y % R::CPR;
+        koff[u] = r * R::RB + (pc ^ R::key(r)) * 16;
+        voff[u] = r * R::RB + (pc ^ R::value(r)) * 16;
+    }
+    // First row of this wavefront's stage of tile m.
+    auto stage_row = [&](int m) { return row_last - m * step + (S::OWN ? w * KB : 0); };
+    // The stage that is fetched next: its first row's address in each table, how
+    // many rows the prefix has from there on, and its place.
+    const int64_t row_first = h * p.pcap + stage_row(0);
+    const uint8_t *kat = (const uint8_t *)p.k_prefix + row_first * R::RB;
+    const uint8_t *vat = (const uint8_t *)p.v_prefix + row_first * R::RB;
+    const uint8_t *kbat = p.k_prefix_exp + row_first, *vbat = p.v_prefix_exp + row_first;
+    // The bytes of a stage for all: 64 rows a wavefront, the keys' by one half of
+    // them, the values' by the other (some of them the same ones).
+    const int byte_row = 64 * (w % (WAVES / 2) % (S::SR / 64)) + lane;
+    if (Q && !S::OWN) kbat = w >= WAVES / 2 ? vbat : kbat;
+    int left = plen - stage_row(0);
+    unsigned char *to = ring;
+    auto fetch16 = [&](u32x4 rsrc, int off, void *lds_at) __attribute__((always_inline)) {
+        if (ONCE) {
+            lds_fetch16_once(rsrc, off, lds_at);
+        } else {
+            lds_fetch16(rsrc, off, lds_at);
+        }
+    };
+    // Fetches it; rows behind the prefix read as zeros.
+    auto fetch = [&]() __attribute__((always_inline)) {
+        const int rows = min(max(left, 0), S::SR);
+        const u32x4 rk = raw_rsrc(kat, rows * R::RB), rv = raw_rsrc(vat, rows * R::RB);
+#pragma unroll
+        for (int u = 0; u < S::KI; ++u) fetch16(rk, koff[u], to + 1024 * (S::OWN ? u : u * WAVES + w));
+#pragma unroll
+        for (int u = 0; u < S::KI; ++u) fetch16(rv, voff[u], to + S::TABLE + 1024 * (S::OWN ? u : u * WAVES + w));
+        if constexpr (Q) {
+            unsigned char *const bytes = to + 2 * S::TABLE;
+            if constexpr (S::OWN) {
+                const u32x4 bk = raw_rsrc(kbat, rows), bv = raw_rsrc(vbat, rows);
+                if (lane < S::SR) {
+                    lds_fetch1(bk, lane, bytes);
+                    lds_fetch1(bv, lane, bytes + 4 * S::SR);
+                }
+            } else {
+                lds_fetch1(raw_rsrc(kbat, rows), byte_row, bytes + 4 * (byte_row - lane + (w >= WAVES / 2 ? S::SR : 0)));
+            }
+            kbat -= step;
+            vbat -= step;
+        }
+        kat -= (int64_t)step * R::RB;
+        vat -= (int64_t)step * R::RB;
+        left += step;
+        to += S::STAGE;
+        to = to == ring + NST * S::STAGE ? ring : to;
+    };
+#pragma unroll
+    for (int m = 0; m < NST - 1; ++m)
+        if (m < mine) fetch();
+    if (!S::OWN && tid == 0) s_cleaned = 0;   // before the first stage's barrier
+
     // Where the window of a sequence begins; INT32_MAX for none.
     auto low_of = [&](int s) {
         if (s >= d.S) return INT32_MAX;
         const int n = d.len_in[s];
-        return n >= 0 && n < d.cap ? window_lo(p.plen + n, d.k) : INT32_MAX;
+        return n >= 0 && n < d.cap ? window_lo(plen + n, d.k) : INT32_MAX;
     };
     // Over the tile's sequences that meet the chunk: where the first window
     // begins, and the last.
@@ -305,193 +544,311 @@ __global__ __launch_bounds__(NT, TR * D > 64 * 128 ? 1 : 2) void prefix_kernel(C
     for (int i = 0; i < QT; i += 64) {
         const int a = i + lane < QT ? low_of(qt * QT + i + lane) : INT32_MAX;
         lo_min = min(lo_min, a);
-        if (a < end) lo_max = max(lo_max, a);
+        if (a < reach) lo_max = max(lo_max, a);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        lo_min = min(lo_min, __shfl_xor(lo_min, o));
-        lo_max = max(lo_max, __shfl_xor(lo_max, o));
+    lo_min = wave_extreme<false>(lo_min);
+    lo_max = wave_extreme<true>(lo_max);
+    if (lo_min >= reach) {   // nothing for anybody, once the loads have landed
+        wait_loads<0>();
+        return;
     }
-    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
-    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-    if (lo_min >= end) return;
+    const int tiles = (row_last + S::TR - 1 - lo_min) / step + 1;   // that some window meets
 
-    const int s = qt * QT + qg * QB + c;
-    const int lo = low_of(s);
+    int lo[NG];
+    float bias[NG], m[NG], l[NG];
     M mm;
-    mm.clear();
-    float bias = 0.0f;
-    if (s < d.S) {
-        mm.query((const T *)d.q_new + ((int64_t)s * d.H + h) * D, g);
-        bias = fusion_bias(d.gate[s * d.gss + h * d.gsh], true).local;
-    } else {
-        mm.clear_query();
-    }
-    const float c2 = d.scale * kLog2e;
-    const bool clamped = d.clamp > 0.0f;
-
-    float m = -INFINITY, l = 0.0f;
-    const int row0 = row_begin + max(lo_min - row_begin, 0) / TR * TR;
-    if (tid < 2) s_bad[tid] = 0;
-    Stage<T, ST, D, TR> stage;
-    stage.fetch(p, h, row0, end, tid);
-    __syncthreads();
-    int turn = 0;
-    for (int row = row0; row < end; row += TR, turn ^= 1) {
-        const bool masked = row < lo_max;   // some sequence's window begins behind the tile's first row
-        if (stage.put(kt, vt, row, end, tid) && masked) s_bad[turn] = 1;
-        __syncthreads();
-        if (row + TR < end) stage.fetch(p, h, row + TR, end, tid);
-        const bool bad = masked && s_bad[turn];
-        if (tid == 0) s_bad[turn ^ 1] = 0;
+    const int s0 = qt * QT + qg * NG * QB + c;   // this lane's queries: s0, s0 + QB
 #pragma unroll
-        for (int b = 0; b < TR / KB / RS; ++b) {
-            const int blk = b * RS + rs, j0 = row + blk * KB;
-            // rows of the block that the group's sequences meet
-            if (j0 >= end || !__builtin_amdgcn_ballot_w64(lo < min(j0 + KB, end))) continue;
-            const unsigned char *kb = kt + blk * KB * M::KROW, *vb = vt + blk * KB * M::VROW;
-            float sc[M::NS];
-            mm.scores(kb, c, g, sc);
-            if (clamped) {
+    for (int n = 0; n < NG; ++n) {
+        const int s = s0 + n * QB;
+        lo[n] = low_of(s);
+        mm.query(n, (const T *)d.q_new + ((int64_t)s * d.H + h) * D, g, s < d.S);
+        bias[n] = s < d.S ? fusion_bias(d.gate[s * d.gss + h * d.gsh], true).local : 0.0f;
+        m[n] = -INFINITY;
+        l[n] = 0.0f;
+    }
+    // The queries are waited for here: left to the compiler, the wait stands where
+    // they are used first, in the loop, and there it is for the stages, too.
+    mm.query_landed();
+    int lo_first = lo[0];
+#pragma unroll
+    for (int n = 1; n < NG; ++n) lo_first = min(lo_first, lo[n]);
+    const bool clamped = d.clamp > 0.0f;
+    const float c2 = clamped ? 1.0f : d.scale * kLog2e;   // to log2 units
+
+    // Zeros for the values of a block that are not finite.  Wavefronts that share
+    // the block may all do so: each has written its zeros before it reads.
+    bool cleaned = false;   // wave-uniform
+    auto clean = [&](unsigned char *vb, unsigned *vbytes) {
+        cleaned = true;
+        if (!S::OWN) s_cleaned = 1;
+#pragma unroll 1
+        for (int i = 0; i < KB * R::RB / 1024; ++i) {
+            uint4 v = lds16(vb + 1024 * i + 16 * lane);
+            v.x &= ~R::not_finite(v.x), v.y &= ~R::not_finite(v.y), v.z &= ~R::not_finite(v.z), v.w &= ~R::not_finite(v.w);
+            *reinterpret_cast<uint4 *>(vb + 1024 * i + 16 * lane) = v;
+        }
+        if (Q && lane < KB && vbytes[lane] >= 247) vbytes[lane] = 0;
+    };
+
+    // One block: rows [j0, j0 + KB), rows [blk * KB, + KB) of the stage at kt.
+    auto block = [&](unsigned char *stage, int blk, int j0) __attribute__((always_inline)) {
+        unsigned char *kb = stage + blk * KB * R::RB, *vb = kb + S::TABLE;
+        unsigned *kbytes = reinterpret_cast<unsigned *>(stage + 2 * S::TABLE) + blk * KB, *vbytes = kbytes + S::SR;
+        const bool masked = j0 < lo_max;   // some sequence's window begins behind the block's first row
+        if (masked) {
+            unsigned bad = 0;
+#pragma unroll
+            for (int i = 0; i < KB * R::RB / 1024; ++i) {
+                const uint4 v = lds16(vb + 1024 * i + 16 * lane);
+                bad |= R::not_finite(v.x) | R::not_finite(v.y) | R::not_finite(v.z) | R::not_finite(v.w);
+            }
+            // a code's value past the largest float: 256 * 2^120
+            const bool past = Q && lane < KB && vbytes[lane] >= 247;
+            if (__builtin_amdgcn_ballot_w64(bad || past)) clean(vb, vbytes);
+        }
+        // Every operand is on its way from LDS before the first is used.
+        const unsigned kbyte = Q ? kbytes[c] : 0;
+        uint4 vbyte[Q ? M::NS / 4 : 1];
+        mm.read_keys(kb, c, g);
+        if constexpr (Q) {
+#pragma unroll
+            for (int i = 0; i < M::NS / 4; ++i)
+                vbyte[i] = *reinterpret_cast<const uint4 *>(vbytes + M::slot_row(4 * i, g));
+        }
+        mm.read_values(vb, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        float sc[NG][M::NS];
+        mm.scores(e4m3_scale(kbyte), sc);
+        if (clamped) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
 #pragma unroll
                 for (int i = 0; i < M::NS; ++i)
-                    sc[i] = fminf(fmaxf(sc[i] * d.scale + bias, -d.clamp), d.clamp) * kLog2e;
-            } else {
+                    sc[n][i] = fminf(fmaxf(sc[n][i] * d.scale + bias[n], -d.clamp), d.clamp) * kLog2e;
+        }
+        if (masked || j0 + KB > plen) {
 #pragma unroll
-                for (int i = 0; i < M::NS; ++i) sc[i] *= c2;
-            }
-            if (j0 < lo_max || j0 + KB > end) {
+            for (int n = 0; n < NG; ++n)
 #pragma unroll
                 for (int i = 0; i < M::NS; ++i) {
                     const int j = j0 + M::slot_row(i, g);
-                    sc[i] = j >= lo && j < end ? sc[i] : -INFINITY;
+                    sc[n][i] = j >= lo[n] && j < plen ? sc[n][i] : -INFINITY;
                 }
-            }
-            float mx = sc[0];
+        }
+        float mx[NG];
+        bool raised = false;
 #pragma unroll
-            for (int i = 1; i < M::NS; ++i) mx = fmaxf(mx, sc[i]);
-            mx = query_max<QB>(mx);
-            if (__builtin_amdgcn_ballot_w64(mx > m)) {
-                const float m_new = fmaxf(m, mx);
-                const float alpha = mx > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;
-                m = m_new;
-                l *= alpha;
-                mm.scale(alpha);
+        for (int n = 0; n < NG; ++n) {
+            mx[n] = sc[n][0];
+#pragma unroll
+            for (int i = 1; i < M::NS; ++i) mx[n] = fmaxf(mx[n], sc[n][i]);
+            mx[n] = query_max<QB>(mx[n]) * c2;
+            raised |= mx[n] > m[n];
+        }
+        if (__builtin_amdgcn_ballot_w64(raised)) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                const float m_new = fmaxf(m[n], mx[n]);
+                const float alpha = mx[n] > m[n] ? __builtin_amdgcn_exp2f(m[n] - m_new) : 1.0f;
+                m[n] = m_new;
+                l[n] *= alpha;
+                mm.scale(n, alpha);
             }
-            const float m_use = m == -INFINITY ? 0.0f : m;
+        }
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            const float m_use = m[n] == -INFINITY ? 0.0f : m[n];
 #pragma unroll
             for (int i = 0; i < M::NS; ++i) {
-                sc[i] = __builtin_amdgcn_exp2f(sc[i] - m_use);
-                l += sc[i];
+                sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c2, -m_use));
+                l[n] += sc[n][i];
             }
-            if (!bad) {
-                mm.values(vb, lane, sc);
-            } else {
-                // Row by row, for the sequences whose window holds it.
+        }
+        if constexpr (Q) {
+#pragma unroll
+            for (int i = 0; i < M::NS; i += 4) {
+                const uint4 b = vbyte[i / 4];
+                const float f[4] = {e4m3_scale(b.x), e4m3_scale(b.y), e4m3_scale(b.z), e4m3_scale(b.w)};
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[n][i + e] *= f[e];
+            }
+        }
+        mm.values(sc);
+    };
+
+    unsigned char *stage = ring;
 #pragma unroll 1
-                for (int r = 0; r < KB; ++r) {
-                    // the lane and slot of the query that hold row r
-                    const int gr = (r >> 2) % (64 / QB), ir = (r / (4 * (64 / QB))) * 4 + (r & 3);
-                    float pr = 0.0f;
+    for (int t = 0; t < tiles; ++t) {
+        // Stage t has landed when at most the loads of the stages behind it are on
+        // their way.
+        if (t + NST - 1 <= tiles) {
+            wait_loads<(NST - 2) * S::LOADS>();
+        } else {
+            wait_loads<0>();
+        }
+        // The stage that is fetched next is the one that was read last: by this
+        // wavefront alone, or by all, who are past it at the barrier.
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        if constexpr (!S::OWN) __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        if (t + NST - 1 < tiles) fetch();
+        const int first = stage_row(t);
 #pragma unroll
-                    for (int i = 0; i < M::NS; ++i) {
-                        const float y = __shfl(sc[i], c + QB * gr);
-                        pr = i == ir ? y : pr;
-                    }
-                    pr = M::round(pr);
-                    const int j = j0 + r;
-                    const bool in = j >= lo && j < end;
+        for (int b = 0; b < S::BL; ++b) {
+            const int blk = S::OWN ? 0 : b * RS + rs, j0 = first + blk * KB;
+            // rows that the group's sequences meet
+            if (j0 < plen && __builtin_amdgcn_ballot_w64(lo_first < min(j0 + KB, plen))) block(stage, blk, j0);
+        }
+        stage += S::STAGE;
+        stage = stage == ring + NST * S::STAGE ? ring : stage;
+    }
 #pragma unroll
-                    for (int y = 0; y < M::NO; ++y) {
-                        const T *vr = reinterpret_cast<const T *>(vb + r * M::VROW) + M::ODIM * y + 4 * g;
+    for (int n = 0; n < NG; ++n) l[n] = query_sum<QB>(l[n]);
+
+    if constexpr (!S::OWN) {
+        __syncthreads();
+        cleaned = s_cleaned != 0;
+    }
+    if (cleaned) {
+        // The rows of this wavefront's masked blocks that have values which are not
+        // finite (or too large a scale).
+        const int64_t head = h * p.pcap;
+#pragma unroll 1
+        for (int y = 0; y < tiles * S::BL; ++y) {
+            const int j0 = stage_row(y / S::BL) + (S::OWN ? 0 : (y % S::BL * RS + rs) * KB);
+            if (j0 >= lo_max) continue;
+#pragma unroll 1
+            for (int j = j0; j < min(j0 + KB, plen); ++j) {
+                const ST *kr = (const ST *)p.k_prefix + (head + j) * D, *vr = (const ST *)p.v_prefix + (head + j) * D;
+                const unsigned vbyte = Q ? p.v_prefix_exp[head + j] : 127;
+                unsigned bad = 0;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mm.at(y, e) = in ? mm.at(y, e) + pr * (float)vr[e] : mm.at(y, e);
+                for (int i = 0; i < R::RB; i += 256)
+                    bad |= R::not_finite(reinterpret_cast<const unsigned *>(vr)[(i / 4 + lane) % (R::RB / 4)]);
+                const bool past = Q && vbyte >= 247;
+                if (!past && !__builtin_amdgcn_ballot_w64(bad != 0)) continue;
+#pragma unroll
+                for (int n = 0; n < NG; ++n) {
+                    float sc = query_sum<QB>(mm.dot(n, kr, g));
+                    if constexpr (Q) sc *= e4m3_scale(p.k_prefix_exp[head + j]);
+                    if (clamped) sc = fminf(fmaxf(sc * d.scale + bias[n], -d.clamp), d.clamp) * kLog2e;
+                    const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(sc, c2, -m[n]));
+                    const bool in = j >= lo[n];
+#pragma unroll
+                    for (int z = 0; z < M::NO; ++z) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = element(vr[M::ODIM * z + 4 * g + e]);
+                            const bool there = in && (past || !(fabsf(v) < INFINITY));
+                            mm.at(n, z, e) += there ? pr * (Q ? e4m3_scale(vbyte) * v : v) : 0.0f;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);   // few registers at a time
                     }
                 }
             }
         }
+    }
+
+    // The states of the RS wavefronts of the same queries, joined on the way out:
+    // through LDS, so that the parts are written in whole lines.
+    wait_loads<0>();   // stages that nobody needed
+    constexpr int QUADS = D / 4;
+    float *const o_at = reinterpret_cast<float *>(lds);                             // [wavefront][query][PITCH]
+    float4 *const ml_at = reinterpret_cast<float4 *>(o_at + WAVES * QB * S::PITCH);   // [wavefront][query]
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
         __syncthreads();
-    }
-    l = query_sum<QB>(l);
-
-    // The states of the RS wavefronts of a group of queries, joined by the first.
-    if constexpr (RS > 1) {
-        float *mine = reinterpret_cast<float *>(lds) + ((rs - 1) * G + qg) * (STATE / 4) + lane;
-        if (rs > 0) {
 #pragma unroll
-            for (int y = 0; y < M::NO; ++y)
+        for (int y = 0; y < M::NO; ++y) {
+            f32x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) mine[64 * (4 * y + e)] = mm.at(y, e);
-            mine[64 * (4 * M::NO)] = m;
-            mine[64 * (4 * M::NO + 1)] = l;
+            for (int e = 0; e < 4; ++e) v[e] = mm.at(n, y, e);
+            *reinterpret_cast<f32x4 *>(o_at + (w * QB + c) * S::PITCH + M::ODIM * y + 4 * g) = v;
         }
+        if (g == 0) ml_at[w * QB + c] = make_float4(m[n], l[n], __int_as_float(lo[n]), 0.0f);
         __syncthreads();
-        if (rs > 0) return;
-        float all = m;
-        const float *theirs = reinterpret_cast<const float *>(lds) + qg * (STATE / 4) + lane;
+#pragma unroll 4
+        for (int i = tid; i < G * QB * QUADS; i += NT) {
+            const int q = i / QUADS, quad = i % QUADS;   // of wavefront r * G + q / QB
+            if (__float_as_int(ml_at[q].z) >= reach) continue;   // no window here, or no sequence
+            float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < RS - 1; ++r) all = fmaxf(all, theirs[r * G * (STATE / 4) + 64 * (4 * M::NO)]);
-        const float all_use = all == -INFINITY ? 0.0f : all;
-        const float a = __builtin_amdgcn_exp2f(m - all_use);
-        m = all;
-        l *= a;
-        mm.scale(a);
+            for (int r = 0; r < RS; ++r) top = fmaxf(top, ml_at[r * G * QB + q].x);
+            const float use = top == -INFINITY ? 0.0f : top;
+            f32x4 sum = {};
+            float total = 0.0f;
 #pragma unroll
-        for (int r = 0; r < RS - 1; ++r) {
-            const float *from = theirs + r * G * (STATE / 4);
-            const float f = __builtin_amdgcn_exp2f(from[64 * (4 * M::NO)] - all_use);
-            l += f * from[64 * (4 * M::NO + 1)];
-#pragma unroll
-            for (int y = 0; y < M::NO; ++y)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mm.at(y, e) += f * from[64 * (4 * y + e)];
+            for (int r = 0; r < RS; ++r) {
+                const float4 ml = ml_at[r * G * QB + q];
+                const float f = __builtin_amdgcn_exp2f(ml.x - use);
+                total += f * ml.y;
+                sum += f * *reinterpret_cast<const f32x4 *>(o_at + (r * G * QB + q) * S::PITCH + 4 * quad);
+            }
+            const int s = qt * QT + (q / QB * NG + n) * QB + q % QB;
+            const int64_t at = (int64_t)x * d.S * d.H + (int64_t)s * d.H + h;
+            *reinterpret_cast<f32x4 *>(p.part_o + at * D + 4 * quad) = sum;
+            if (quad == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(top, total);
         }
     }
-    if (lo >= end) return;   // no window here, or no sequence
-    const int64_t at = (int64_t)x * d.S * d.H + (int64_t)s * d.H + h;
-#pragma unroll
-    for (int y = 0; y < M::NO; ++y) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = mm.at(y, e);
-        *reinterpret_cast<f32x4 *>(p.part_o + at * D + M::ODIM * y + 4 * g) = v;
+}
+
+// Calls f with the Shape for a problem: one work-group for all sequences as far
+// as that goes.  Two groups of queries a wavefront share what the rows' operands
+// cost, where their registers leave two wavefronts a SIMD (D = 128: bf16 needs
+// more than 256 a lane, and one wavefront a SIMD is slower than two of one group;
+// float32 in the larger work-groups, too).
+template <typename T, typename ST, int D, typename F>
+auto with_queries(int S, F f) {
+    constexpr int QB = Mma<T, ST, D, 1>::QB;
+    if (S <= QB) return f(Shape<T, ST, D, 1, 1>());
+    if constexpr (D == 64) {
+        if (S <= 2 * QB) return f(Shape<T, ST, D, 1, 2>());
+        return S <= 4 * QB ? f(Shape<T, ST, D, 2, 2>()) : f(Shape<T, ST, D, 4, 2>());
+    } else {
+        if (S <= 2 * QB) {
+            if constexpr (sizeof(T) == 4) return f(Shape<T, ST, D, 1, 2>());
+            else return f(Shape<T, ST, D, 2, 1>());
+        }
+        if constexpr (sizeof(T) == 4) {
+            if (S > 4 * QB) return f(Shape<T, ST, D, 8, 1>());
+        }
+        return f(Shape<T, ST, D, 4, 1>());
     }
-    if (g == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(m, l);
 }
 
-template <typename T, typename ST, int D, int G, int TR>
-hipError_t launch_g(const CachedParams &p, hipStream_t stream) {
-    constexpr int QT = Mma<T, D>::QB * G;
-    const int n_qt = (p.d.S + QT - 1) / QT;
-    const int64_t n = (int64_t)p.d.H * p.chunks * n_qt;
-    return launch_kernel(prefix_kernel<T, ST, D, G, TR>, dim3((unsigned)xcd_grid(n)), dim3(NT), stream, p, n_qt,
-                         (uint32_t)n);
+template <typename T, typename ST, typename F>
+auto with_dim(const CachedParams &p, F f) {
+    return p.d.D == 64 ? with_queries<T, ST, 64>(p.d.S, f) : with_queries<T, ST, 128>(p.d.S, f);
 }
 
-template <typename T, typename ST, int D>
-hipError_t launch_d(const CachedParams &p, hipStream_t stream) {
-    constexpr int QB = Mma<T, D>::QB;
-    constexpr int FEW = sizeof(T) == 2 ? 128 : 64;   // rows of a tile that four wavefronts share
-    if (p.d.S <= QB) return launch_g<T, ST, D, 1, FEW>(p, stream);
-    if (p.d.S <= 2 * QB) return launch_g<T, ST, D, 2, 64>(p, stream);
-    return launch_g<T, ST, D, 4, 64>(p, stream);
-}
-
-template <typename T, typename ST>
-hipError_t launch_t(const CachedParams &p, hipStream_t stream) {
-    return p.d.D == 64 ? launch_d<T, ST, 64>(p, stream) : launch_d<T, ST, 128>(p, stream);
+template <typename F>
+auto with_shape(const CachedParams &p, bool bf16, F f) {
+    if (p.k_prefix_exp) return bf16 ? with_dim<__bf16, e4m3>(p, f) : with_dim<float, e4m3>(p, f);
+    return bf16 ? with_dim<__bf16, __bf16>(p, f) : with_dim<float, float>(p, f);
 }
 
 }  // namespace
 
-PrefixShape prefix_shape(int S, bool bf16) {
-    const int QB = bf16 ? 32 : 16;
-    return PrefixShape{S <= QB ? QB : S <= 2 * QB ? 2 * QB : 4 * QB, bf16 && S <= QB ? 128 : 64};
+constexpr int64_t kKeepPrefix = 64 << 20;
+
+PrefixShape prefix_shape(const CachedParams &p, bool bf16) {
+    return with_shape(p, bf16, [](auto s) {
+        using S = decltype(s);
+        return PrefixShape{S::QT, S::TR, S::TWO ? 2 : 1};
+    });
 }
 
 hipError_t launch_prefix(const CachedParams &p, bool bf16, hipStream_t stream) {
-    if (p.k_prefix_exp) return bf16 ? launch_t<__bf16, e4m3>(p, stream) : launch_t<float, e4m3>(p, stream);
-    return bf16 ? launch_t<__bf16, __bf16>(p, stream) : launch_t<float, float>(p, stream);
+    return with_shape(p, bf16, [&](auto s) {
+        using S = decltype(s);
+        const int n_qt = (p.d.S + S::QT - 1) / S::QT;
+        const int64_t n = (int64_t)p.d.H * p.chunks * n_qt;
+        const bool once = n_qt == 1 && 2 * (int64_t)p.d.H * p.near * S::R::RB > kKeepPrefix;
+        return launch_kernel(once ? prefix_kernel<S, true> : prefix_kernel<S, false>, dim3((unsigned)xcd_grid(n)), dim3(S::NT), stream, p, n_qt, (uint32_t)n);
+    });
 }
 
 }  // namespace pi_attn
