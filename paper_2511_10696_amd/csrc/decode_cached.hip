@@ -101,10 +101,6 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     const int sub = lane % LPR, rg = lane / LPR;
     T *out = (T *)d.out + sh * D;
 
-    // What waits for no length is on its way with it: the query, and of the parts
-    // the one that this row group joins first (of a chunk that the window does not
-    // meet it holds anything, and is left out below).
-    constexpr bool PARTS = MODE == WHOLE || MODE == JOIN;
     constexpr int WIDE = EPL * (int)sizeof(T) / 16;   // loads of a lane's elements in the working type
     const int n = d.len_in[s];   // own rows
     auto load_wide = [&](const void *row, uint4 (&u)[WIDE]) __attribute__((always_inline)) {
@@ -113,16 +109,6 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     };
     uint4 qw[WIDE];
     if constexpr (MODE != JOIN) load_wide(d.q_new, qw);
-    const int parts = PARTS ? p.chunks + (MODE == JOIN ? p.own_parts : 0) : 0;
-    float2 ml = make_float2(0.0f, 0.0f);
-    uint4 po[EPL / 4];
-    auto load_part = [&](int x) __attribute__((always_inline)) {
-        const int64_t at = (int64_t)min(x + rg, parts - 1) * n_sh + sh;
-        ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
-#pragma unroll
-        for (int i = 0; i < EPL / 4; ++i) po[i] = ld16(p.part_o + at * D + sub * EPL + 4 * i);
-    };
-    if (PARTS && w * RPI < parts) load_part(w * RPI);
     const FusionBias fb = fusion_bias(d.gate[s * d.gss + h * d.gsh], CLAMP);
 
     if (n < 0 || n >= d.cap) {
@@ -311,20 +297,31 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
 
     // The parts: of the prefix chunks that this window meets, and (JOIN) of the
     // ranges of own rows.
+    // (Loaded before the rows they would be there by now, and cost the registers of
+    // a wavefront a SIMD: 40 us as it is, 43 so, 64 sequences of 32 heads behind
+    // 4096 e4m3 rows, 128 own ones.)
+    const int parts = MODE == WHOLE || MODE == JOIN ? p.chunks + (MODE == JOIN ? p.own_parts : 0) : 0;
     for (int x = w * RPI; x < parts; x += WAVES * RPI) {
-        if (x != w * RPI) load_part(x);
         const int y = x + rg;
         const bool there = y < parts && (y >= p.chunks || (lo < p.plen && lo < chunk_end(p, y)));
-        const float top = there ? ml.x : -INFINITY;
-        const float m_use = raise(top);
-        const float f = __builtin_amdgcn_exp2f(top - m_use);
-        l += there ? f * ml.y : 0.0f;
+        const int64_t at = (int64_t)y * n_sh + sh;
+        float2 ml = make_float2(-INFINITY, 0.0f);
+        f32x4 o[EPL / 4];
 #pragma unroll
-        for (int i = 0; i < EPL / 4; ++i) {
-            const f32x4 o = __builtin_bit_cast(f32x4, po[i]);
+        for (int i = 0; i < EPL / 4; ++i) o[i] = f32x4{};
+        if (there) {
+            ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[4 * i + e] += there ? f * o[e] : 0.0f;
+            for (int i = 0; i < EPL / 4; ++i)
+                o[i] = *reinterpret_cast<const f32x4 *>(p.part_o + at * D + sub * EPL + 4 * i);
         }
+        const float m_use = raise(ml.x);
+        const float f = __builtin_amdgcn_exp2f(ml.x - m_use);
+        l += f * ml.y;
+#pragma unroll
+        for (int i = 0; i < EPL / 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[4 * i + e] += f * o[i][e];
     }
 
     // Merge the row groups of the wavefront (lanes with the same sub).
@@ -369,6 +366,8 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     }
 }
 
+// ONCE, by the bytes of a step's window rows, as in decode.hip: they are read
+// once, and kept in the caches they only push out what is there.
 constexpr int64_t kKeepBytes = 12 << 20;
 
 template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH>
@@ -381,25 +380,37 @@ hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
                          dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
 }
 
+// Wavefronts and chunk size, by the load instructions of a window's keys and the
+// launch: a few (s, h) by the chain of one wavefront, a chip full of them by the
+// wavefronts that it holds and by what a work-group costs beside its rows.  us,
+// 8 wavefronts of 4 slots, 4 of 4 and 2 of 4, e4m3, D = 128: 512 (s, h) of 128
+// rows (16 loads) 7.1, 7.1 and 8.0, of 512 rows 13.4, 14.8 (of 2 slots) and 18.0;
+// 2048 of 32 rows 16.4, 8.4 and 7.9, of 128 rows 21.3, 16.8 and 15.2, of 256 rows
+// 29.1, 26.6 and 24.8, of 512 rows 46.8, 47 and 47.4, of 1024 rows 87.0, - and
+// 92.0.  With the parts of a prefix, 2048 (s, h): of 256 rows 44.7, 42.5 and 36.5,
+// of 512 rows 48.0, - and 41.3; bf16 of 256 rows 50.5, - and 48.4.
 template <typename T, typename ST, int D, bool CLAMP>
 hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
     const int rows = std::min(p.d.k, p.d.cap) + (p.direct ? p.near : 0);
     const int loads = (rows + Row<ST, D>::RPI - 1) / Row<ST, D>::RPI;
+    const bool many = n >= 2048;
     if (p.direct) {
-        if (loads > 32) return launch_n<T, ST, D, CLAMP, DIRECT, 8, 4>(p, stream);
-        return launch_n<T, ST, D, CLAMP, DIRECT, 4, 4>(p, stream);
+        return loads > 32 ? launch_n<T, ST, D, CLAMP, DIRECT, 8, 4>(p, stream)
+                          : launch_n<T, ST, D, CLAMP, DIRECT, 4, 4>(p, stream);
     }
     if (p.own_parts) {
         const hipError_t e = launch_n<T, ST, D, CLAMP, RANGE, 4, 4>(p, stream);
         return e != hipSuccess ? e : launch_n<T, ST, D, CLAMP, JOIN, 4, 4>(p, stream);
     }
     if (p.chunks) {
-        if (loads > 32) return launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream);
-        if (loads > 8) return launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
-        return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
+        if (loads <= 8) return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
+        if (many && loads <= 64) return launch_n<T, ST, D, CLAMP, WHOLE, 2, 4>(p, stream);
+        return loads > 32 ? launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream)
+                          : launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
     }
     if (loads > 32) return launch_n<T, ST, D, CLAMP, ALONE, 8, 4>(p, stream);
+    if (many && loads > 2) return launch_n<T, ST, D, CLAMP, ALONE, 2, 4>(p, stream);
     if (loads > 8 || (loads > 4 && n <= 1024)) return launch_n<T, ST, D, CLAMP, ALONE, 4, 4>(p, stream);
     return launch_n<T, ST, D, CLAMP, ALONE, 2, 2>(p, stream);
 }
@@ -413,10 +424,31 @@ hipError_t launch_t(const CachedParams &p, hipStream_t stream) {
 
 }  // namespace
 
-#ifndef DIRECT_EL
-#define DIRECT_EL (4 << 20)
-#endif
-constexpr int64_t kDirectElements = DIRECT_EL;
+// Whether the sequences read the prefix's rows for themselves, in one launch: as
+// long as one (s, h) has a chain of few loads, and all of them together little
+// more than the launch that is saved.  us, by chunks and so: bf16 D = 64, 64
+// (s, h) 1024 rows 8.7 and 7.3, 2048 rows 8.8 and 10.5; D = 128, 128 (s, h) 512
+// rows 9.8 and 7.2, 1024 rows 9.9 and 11.0; e4m3 D = 128, 128 (s, h) 1024 rows
+// 10.3 and 9.7, 2048 rows 10.9 and 15.0; 2048 (s, h): bf16 D = 64 128 rows (67 MB
+// in all) 12.9 and 9.2, 256 rows 13.2 and 15.0; e4m3 D = 64 256 rows (67 MB) 15.3
+// and 13.4, 512 rows 16.0 and 22.2.
+bool read_directly(const CachedParams &p, int element_bytes) {
+    const int64_t bytes = 2 * (int64_t)p.near * p.d.D * element_bytes;   // keys and values of an (s, h)
+    return bytes <= 300 << 10 && (int64_t)p.d.S * p.d.H * bytes <= 100 << 20;
+}
+
+// Ranges of own rows that a step is split into: where a few (s, h) have long
+// chains of loads, which a second launch costs less than; enough for 512
+// work-groups, of 64 KB at least.  us, whole and split, e4m3, D = 128: 32 (s, h)
+// of 1600 rows 13.5 and 11.1, of 16384 rows 99.4 and 27.8; 64 of 2048 17.0 and
+// 13.1, 128 of 2048 18.3 and 18.2; 256 of 2048 24.5 and 28.2, of 8192 80.9 and
+// 85.0; 1024 and 2048 work-groups the same but for 256 (s, h) and one.
+int own_parts(const CachedParams &p, int element_bytes) {
+    const int64_t n = (int64_t)p.d.S * p.d.H, own = std::min(p.d.k, p.d.cap - 1);
+    const int64_t bytes = 2 * own * p.d.D * element_bytes;   // keys and values of an (s, h)
+    if (bytes < 384 << 10 || n > 128) return 0;
+    return (int)std::min<int64_t>(512 / n, bytes >> 16);
+}
 
 // At most `most` chunks of whole tiles, as even as they can be.
 int64_t even_chunks(const CachedParams &p, int64_t most) {
@@ -427,24 +459,27 @@ int64_t even_chunks(const CachedParams &p, int64_t most) {
 // The sizes of the parts, by the problem's sizes alone (the lengths lie in
 // device memory).
 void plan_decode_cached(CachedParams &p, bool bf16) {
-    const int64_t n = (int64_t)p.d.S * p.d.H;
     p.near = std::min(p.d.k, p.plen);
     p.tile = p.chunks = p.own_parts = 0;
-    const int64_t own = std::min(p.d.k, p.d.cap - 1);
-    p.direct = p.near > 0 && n * (p.near + own) * p.d.D <= kDirectElements;
-    if (p.near > 0 && !p.direct) {
-        // the most chunks that any caches' type takes
-        const PrefixShape shape = prefix_shape(p, bf16);
-        p.tile = !bf16 && p.d.S <= 32 ? 64 : 128;
-        const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
+    p.direct = false;
+    if (p.near > 0 && !read_directly(p, bf16 ? 2 : 4)) {
+        // the most chunks that any caches' type takes: of 64 rows, two a CU
+        const int queries = prefix_shape(p, bf16).queries;
+        const int64_t side = (int64_t)p.d.H * ((p.d.S + queries - 1) / queries);
+        p.tile = 64;
         p.chunks = (int)even_chunks(p, std::max<int64_t>(1, 512 / side));
     }
-    if (n < 256 && own >= 4096) p.own_parts = (int)std::min<int64_t>(512 / n, own / 1024);
+    p.own_parts = own_parts(p, bf16 ? 2 : 4);
 }
 
 hipError_t launch_decode_cached(const CachedParams &planned, bool bf16, hipStream_t stream) {
     CachedParams p = planned;
     if ((int64_t)p.d.S * p.d.H == 0) return hipSuccess;
+    if (p.near > 0 && read_directly(p, p.k_exp ? 1 : bf16 ? 2 : 4)) {
+        p.direct = true;
+        p.chunks = 0;
+    }
+    p.own_parts = p.direct ? 0 : own_parts(p, p.k_exp ? 1 : bf16 ? 2 : 4);
     if (p.chunks) {
         const PrefixShape shape = prefix_shape(p, bf16);
         const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);

@@ -134,7 +134,7 @@ hipError_t launch_decode_cached(const CachedParams &p, bool bf16, hipStream_t st
 // Its shared prefix: the parts of the chunks.
 struct PrefixShape {
     int queries;                    // of a work-group
-    int tile;                       // rows that it takes at a time, 128 at most (float32: of <= 16 sequences 64)
+    int tile;                       // rows that it takes at a time, at least 64
     int per_cu;                     // work-groups that share a CU
 };
 PrefixShape prefix_shape(const CachedParams &p, bool bf16);
