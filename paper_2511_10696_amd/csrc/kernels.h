@@ -71,6 +71,8 @@ struct CacheRowsParams {
     int S, H, n, D, cap;
     uint32_t rows;                  // S * H * n, at least 1
     Divisor by_n, by_h;
+    uint32_t runs;                  // of a head, and
+    bool heads_first;               // their order; set by the launch
     void *k, *v;                    // read by a store, written by a load
     int64_t sb, sh, sn;             // element strides shared by k and v
     const int32_t *start, *count;   // [S], or nullptr: 0, n
