@@ -416,17 +416,21 @@ struct Shape {
     static_assert(SR * R::CPR % (64 * (OWN ? 1 : WAVES)) == 0 && BL >= 1 && NST >= 2, "whole loads, whole blocks");
 };
 
-// lds_fetch16 of rows that are not to be kept in the caches.
-__device__ inline void lds_fetch16_once(u32x4 rsrc, int voff, void *lds) {
-    const unsigned m0 = __builtin_amdgcn_readfirstlane(
-        (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
-    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
+// lds_fetch16 to a 32-bit LDS address (a pointer's arithmetic is in 64 bits).
+// ONCE: of rows that are not to be kept in the caches.
+template <bool ONCE>
+__device__ inline void fetch16(u32x4 rsrc, int voff, unsigned lds_at) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(lds_at);
+    if constexpr (ONCE) {
+        asm volatile("buffer_load_dwordx4 %0, %1, 0 offen nt lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
+    } else {
+        asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
+    }
 }
 
-// One byte a lane into the words at lds + 4 * lane.
-__device__ inline void lds_fetch1(u32x4 rsrc, int voff, void *lds) {
-    const unsigned m0 = __builtin_amdgcn_readfirstlane(
-        (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+// One byte a lane into the words at lds_at + 4 * lane.
+__device__ inline void fetch1(u32x4 rsrc, int voff, unsigned lds_at) {
+    const unsigned m0 = __builtin_amdgcn_readfirstlane(lds_at);
     asm volatile("buffer_load_ubyte %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(m0));
 }
 
@@ -490,32 +494,26 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
     const int byte_row = 64 * (w % (WAVES / 2) % (S::SR / 64)) + lane;
     if (Q && !S::OWN) kbat = w >= WAVES / 2 ? vbat : kbat;
     int left = plen - stage_row(0);
-    unsigned char *to = ring;
-    auto fetch16 = [&](u32x4 rsrc, int off, void *lds_at) __attribute__((always_inline)) {
-        if (ONCE) {
-            lds_fetch16_once(rsrc, off, lds_at);
-        } else {
-            lds_fetch16(rsrc, off, lds_at);
-        }
-    };
+    const unsigned ring_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)ring;
+    unsigned to = ring_at;
     // Fetches it; rows behind the prefix read as zeros.
     auto fetch = [&]() __attribute__((always_inline)) {
         const int rows = min(max(left, 0), S::SR);
         const u32x4 rk = raw_rsrc(kat, rows * R::RB), rv = raw_rsrc(vat, rows * R::RB);
 #pragma unroll
-        for (int u = 0; u < S::KI; ++u) fetch16(rk, koff[u], to + 1024 * (S::OWN ? u : u * WAVES + w));
+        for (int u = 0; u < S::KI; ++u) fetch16<ONCE>(rk, koff[u], to + 1024 * (S::OWN ? u : u * WAVES + w));
 #pragma unroll
-        for (int u = 0; u < S::KI; ++u) fetch16(rv, voff[u], to + S::TABLE + 1024 * (S::OWN ? u : u * WAVES + w));
+        for (int u = 0; u < S::KI; ++u) fetch16<ONCE>(rv, voff[u], to + S::TABLE + 1024 * (S::OWN ? u : u * WAVES + w));
         if constexpr (Q) {
-            unsigned char *const bytes = to + 2 * S::TABLE;
+            const unsigned bytes = to + 2 * S::TABLE;
             if constexpr (S::OWN) {
                 const u32x4 bk = raw_rsrc(kbat, rows), bv = raw_rsrc(vbat, rows);
                 if (lane < S::SR) {
-                    lds_fetch1(bk, lane, bytes);
-                    lds_fetch1(bv, lane, bytes + 4 * S::SR);
+                    fetch1(bk, lane, bytes);
+                    fetch1(bv, lane, bytes + 4 * S::SR);
                 }
             } else {
-                lds_fetch1(raw_rsrc(kbat, rows), byte_row, bytes + 4 * (byte_row - lane + (w >= WAVES / 2 ? S::SR : 0)));
+                fetch1(raw_rsrc(kbat, rows), byte_row, bytes + 4 * (byte_row - lane + (w >= WAVES / 2 ? S::SR : 0)));
             }
             kbat -= step;
             vbat -= step;
@@ -524,7 +522,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
         vat -= (int64_t)step * R::RB;
         left += step;
         to += S::STAGE;
-        to = to == ring + NST * S::STAGE ? ring : to;
+        to = to == ring_at + NST * S::STAGE ? ring_at : to;
     };
 #pragma unroll
     for (int m = 0; m < NST - 1; ++m)
