@@ -300,6 +300,11 @@ int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int
  *                quantised.
  *   k, pi, len_out, q_new, k_new, v_new, gate ... lse   as pi_attn_decode_step.
  *   work         as pi_attn_decode_step_e4m3, for plen.
+ * The prefix must not overlap rows that the step writes.  Which kernels run
+ * depends on the sizes alone, the sums are taken in a fixed order: the same call
+ * gives the same bits.  A small prefix is read by every sequence for itself, in
+ * one launch; otherwise its rows are taken in chunks, on the matrix cores, and
+ * joined with the own rows by a second launch.
  * A length outside [0, cap): NaN for that sequence's outputs, its caches
  * untouched, len_out[s] = len_in[s].  bf16: the weights of the prefix rows
  * enter their value product as bf16.

@@ -741,11 +741,16 @@ def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, ou
     return out, strides
 
 
-def _workspace(torch, work, dtype, S, H, D, plen, cap, k, device):
+def _workspace(torch, work, dtype, S, H, D, plen, cap, k, device, stream):
     """The caller's workspace (checked), a new one, or None where none is needed."""
     need = int(library().pi_attn_decode_workspace(_dtype_code(dtype), S, H, D, plen, cap, int(k)))
     if work is None:
-        return torch.empty(need, dtype=torch.float32, device=device) if need > 0 else None
+        if need <= 0:
+            return None
+        work = torch.empty(need, dtype=torch.float32, device=device)
+        if stream is not None:   # let go at the return, it must not be handed out again before the step is done
+            work.record_stream(stream)
+        return work
     if work.dtype != torch.float32 or not work.is_contiguous() or work.numel() < need:
         raise ValueError(f"work must be a contiguous float32 tensor of at least {need} elements")
     return work
@@ -769,7 +774,7 @@ def pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_ex
     _same_device(*ts)
     S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
     out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
-    work = _workspace(torch, work, q_new.dtype, S, H, D, 0, cap, k, q_new.device)
+    work = _workspace(torch, work, q_new.dtype, S, H, D, 0, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_e4m3(
             _dtype_code(q_new.dtype), S, H, D, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out), _ptr(q_new),
@@ -827,7 +832,7 @@ def pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, 
                     plen > 1 and t.stride(1) != 1 or H > 1 and plen > 0 and t.stride(0) != pcap):
                 raise ValueError(f"{name} must be a uint8 [H, plen] tensor that lies as the rows of k_prefix do")
     out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
-    work = _workspace(torch, work, q_new.dtype, S, H, D, plen, cap, k, q_new.device)
+    work = _workspace(torch, work, q_new.dtype, S, H, D, plen, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_prefix(
             _dtype_code(q_new.dtype), S, H, D, plen, pcap, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out),

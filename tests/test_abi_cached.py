@@ -63,7 +63,8 @@ def test_rows_empty_is_noop(lib, call, kw):
     assert call(lib, **kw) == 0
 
 
-BASE = dict(dtype=1, S=2, H=3, D=64, plen=100, pcap=100, cap=20, k=500, pi=0, li=16, lo=None, q=16, kn=16, vn=16, kp=16,
+# A prefix and windows that need a workspace.
+BASE = dict(dtype=1, S=2, H=3, D=64, plen=20000, pcap=20000, cap=20, k=30000, pi=0, li=16, lo=None, q=16, kn=16, vn=16, kp=16,
             vp=16, kpe=1, vpe=1, kc=16, vc=16, ke=1, ve=1, gate=16, gss=0, gsh=1, scale=0.125, clamp=0.0, out=16, lse=None,
             work=16, stream=None)
 
@@ -117,7 +118,7 @@ def test_e4m3_needs_bytes(lib):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(plen=-1), EINVAL), (dict(pcap=99), EINVAL), (dict(kp=None), EINVAL), (dict(vp=None), EINVAL),
+    (dict(plen=-1), EINVAL), (dict(pcap=19999), EINVAL), (dict(kp=None), EINVAL), (dict(vp=None), EINVAL),
     (dict(kp=24), EINVAL), (dict(kpe=None), EINVAL), (dict(vpe=None), EINVAL), (dict(ke=None, ve=None), EINVAL),
     (dict(ke=None, ve=None, kpe=None), EINVAL), (dict(plen=(1 << 31) - 100, pcap=(1 << 31) - 100), EUNSUP),
 ])
@@ -128,16 +129,17 @@ def test_prefix_rejects(lib, kw, code):
 def test_workspace_size(lib):
     need = pa.pi_attn_decode_workspace
     bf = torch.bfloat16
-    assert need(bf, 2, 3, 64, 0, 100, 50) == 0 and need(bf, 0, 3, 64, 100, 100, 50) == 0
-    assert need(bf, 2, 3, 64, 100, 100, 0) == 0   # no window rows in the prefix
+    assert need(bf, 2, 3, 64, 0, 100, 50) == 0 and need(bf, 0, 3, 64, 100000, 100, 50000) == 0
+    assert need(bf, 2, 3, 64, 100000, 100, 0) == 0   # no window rows in the prefix
+    assert need(bf, 2, 3, 64, 200, 100, 300) == 0    # few of them: no parts
     for dtype in (bf, torch.float32):
         for D in (64, 128):
-            for S, H, plen, cap, k in ((1, 1, 1, 1, 1), (4, 8, 5000, 10, 6000), (200, 32, 70000, 10, 80000), (1, 2, 0, 9000, 9000),
-                                       (1, 1, 2 ** 30, 2 ** 30 - 5000, 2 ** 31 - 1), (4000, 4000, 9, 9, 9)):
+            for S, H, plen, cap, k in ((4, 8, 5000, 10, 6000), (200, 32, 70000, 10, 80000), (1, 2, 0, 9000, 9000), (1, 1, 3000, 5, 4000),
+                                       (1, 1, 2 ** 30, 2 ** 30 - 5000, 2 ** 31 - 1), (4000, 4000, 64, 9, 64)):
                 n = need(dtype, S, H, D, plen, cap, k)
                 assert n > 0 and n % (S * H * (D + 2)) == 0
-                # a part is at least a tile of rows, and what they take stays small
-                assert n // (S * H * (D + 2)) <= max(1, (min(k, plen) + 63) // 64 + min(k, cap) // 1024)
+                # a part is at least a tile of rows, or 64 KB of own ones, and they are few
+                assert n // (S * H * (D + 2)) <= (min(k, plen) + 63) // 64 + 8 * min(k, cap) * D // 65536
                 assert n // (S * H * (D + 2)) <= 1024
     for bad in ((2, 3, 96, 0, 10, 5), (-1, 3, 64, 0, 10, 5), (2, 3, 64, -1, 10, 5), (2, 3, 64, 0, 0, 5), (2, 3, 64, 0, 9, -1),
                 (1 << 12, 1 << 12, 64, 0, 9, 9), (1, 1, 64, 1 << 30, 1 << 30, 4)):

@@ -177,12 +177,12 @@ def test_no_prefix_rows(device, dtype, quant):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("quant", [False, True])
-@pytest.mark.parametrize("S", [5, 50])
-def test_masked_rows_that_are_not_finite(device, dtype, quant, S):
+@pytest.mark.parametrize("S,D,H", [(5, 64, 2), (50, 64, 2), (20, 128, 80), (50, 128, 40), (100, 128, 20), (140, 64, 20)])
+def test_masked_rows_that_are_not_finite(device, dtype, quant, S, D, H):
     """A prefix row with NaN and infinities in the windows of some sequences only: those get NaN, the others their values."""
     plen, k, cap = 300, 200, 150
     lens = [(i * 29) % cap for i in range(S)]
-    p = Problem(dtype, quant, S, 2, 64, plen, cap, k, 0, lens)
+    p = Problem(dtype, quant, S, H, D, plen, cap, k, 0, lens)
     bad = 170   # met by the sequences with plen + n - k <= 170, n <= 70
     clean = p.expected()
     for x in p.shared:
@@ -224,9 +224,10 @@ def test_value_rows_that_are_not_finite(device, quant):
 
 
 @pytest.mark.parametrize("quant", [False, True])
-def test_one_row_dominates(device, quant):
+@pytest.mark.parametrize("plen", [400, 4000])
+def test_one_row_dominates(device, quant, plen):
     """A prefix row with nearly all of the weight: its value row, to the output's rounding."""
-    p = Problem(torch.bfloat16, quant, 20, 2, 64, 400, 30, 1000, 0, [i % 30 for i in range(20)])
+    p = Problem(torch.bfloat16, quant, 20, 2, 64, plen, 30, 5000, 0, [i % 30 for i in range(20)])
     q = p.q.float()
     key = torch.where(q[:1] > 0, 40.0, -40.0)
     p.q.copy_(torch.sign(q[:1]).expand_as(q))   # every sequence asks for the same row
@@ -329,3 +330,137 @@ def test_from_prompt_to_steps(device):
         assert float((a.float() - b.float()).abs().max()) <= 3 * 2.0 ** -8 * 5
         for x, y in ((oc[0], fc[0]), (oc[1], fc[1])):
             assert torch.equal(x.view(torch.uint8)[:, :, :i + 1], y.view(torch.uint8)[:, :, plen:plen + i + 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("S,H,D", [(20, 40, 64), (40, 40, 64), (60, 40, 128), (70, 30, 64), (140, 16, 64), (33, 40, 128), (130, 16, 128)])
+def test_prefix_in_chunks(device, dtype, quant, S, H, D):
+    """Prefixes that are taken in chunks: every number of groups of queries, a window in the middle of a tile, some windows
+    that end before the last tile."""
+    plen, cap, k, pi = 700, 40, 600, 640
+    lens = [(7 * s) % cap for s in range(S)]
+    p = Problem(dtype, quant, S, H, D, plen, cap, k, pi, lens, clamp=6.0 if S % 20 else 0.0)
+    assert pa.pi_attn_decode_workspace(dtype, S, H, D, plen, cap, k) > 0
+    p.check()
+
+
+def test_windows_that_have_left_the_prefix(device):
+    """Lengths past the window: no row of the prefix but the partners, whose chunks have nothing to do."""
+    S, H, k = 40, 40, 300
+    Problem(torch.bfloat16, True, S, H, 64, 2000, 700, k, 900, [350 + 8 * s for s in range(S)]).check()
+
+
+@pytest.mark.parametrize("quant", [False, True])
+def test_same_bits_by_the_python_marshalling(device, quant):
+    """A given stream takes the Python marshalling: the same kernels, the same bits, with its own workspace."""
+    mk = lambda: Problem(torch.bfloat16, quant, 33, 40, 128, 700, 40, 600, 640, [s for s in range(33)])
+    a, b = mk(), mk()
+    x = a.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = b.run(stream=side)
+    side.synchronize()
+    assert torch.equal(x, y) and torch.equal(a.lse, b.lse) and torch.equal(a.len_out, b.len_out)
+
+
+def test_refusals(device):
+    """What the binding refuses, each with one thing wrong."""
+    S, H, D, plen, cap = 2, 3, 64, 50, 20
+    p = Problem(torch.bfloat16, True, S, H, D, plen, cap, 30, 0, [1, 2])
+    before = [x.view(torch.uint8).clone() for x in p.own]
+
+    def step(**kw):
+        a = dict(len_in=p.lens, q=p.q, kn=p.kn, vn=p.vn, kp=p.shared[0], vp=p.shared[1], kc=p.own[0], vc=p.own[1],
+                 gate=p.gate, kpe=p.shared_exp[0], vpe=p.shared_exp[1], ke=p.own_exp[0], ve=p.own_exp[1], k=30, pi=0, more={})
+        a.update(kw)
+        return pa.pi_attn_decode_step_prefix(a["len_in"], a["q"], a["kn"], a["vn"], a["kp"], a["vp"], a["kc"], a["vc"],
+                                             a["gate"], a["k"], a["pi"], k_prefix_exp=a["kpe"], v_prefix_exp=a["vpe"],
+                                             k_exp=a["ke"], v_exp=a["ve"], **a["more"])
+
+    plain = torch.zeros(S, H, cap, D, device="cuda", dtype=torch.bfloat16)
+    for kw, error in [
+        (dict(ke=None), ValueError), (dict(vpe=None), ValueError), (dict(kpe=p.shared_exp[0].contiguous()), ValueError),
+        (dict(kp=p.shared[0][:, :, ::2]), ValueError), (dict(kp=p.shared[0].contiguous()), ValueError),
+        (dict(kp=p.shared[0][:2]), ValueError), (dict(kc=plain, vc=plain), ValueError), (dict(len_in=p.lens.long()), ValueError),
+        (dict(q=p.q.half()), ValueError), (dict(kn=p.kn.float()), ValueError), (dict(gate=p.gate.double()), TypeError),
+        (dict(gate=torch.zeros(H + 1, device="cuda")), ValueError), (dict(k=-1), pa.PiAttnError), (dict(pi=-1), pa.PiAttnError),
+        (dict(more=dict(scale=0.0)), pa.PiAttnError), (dict(more=dict(logit_clamp=float("nan"))), pa.PiAttnError),
+        (dict(more=dict(len_out=p.lens)), pa.PiAttnError), (dict(more=dict(out=p.q.float())), ValueError),
+        (dict(more=dict(lse=torch.zeros(S, device="cuda"))), ValueError), (dict(more=dict(work=torch.zeros(9))), RuntimeError),
+        (dict(ke=p.own_exp[0].int()), ValueError), (dict(kc=p.own[0].transpose(0, 1)), ValueError),
+    ]:
+        with pytest.raises(error):
+            step(**kw)
+    k = torch.zeros(S, H, 5, D, device="cuda")
+    for args, error in [((k, k.half()), ValueError), ((k.half(), k.half()), TypeError), ((k[:, :, :, :32], k[:, :, :, :32]), ValueError),
+                        ((k[:1], k[:1]), ValueError), ((k, k.transpose(0, 1).contiguous().transpose(0, 1)), ValueError)]:
+        with pytest.raises(error):
+            pa.pi_attn_cache_store(*args, *p.own, *p.own_exp)
+    with pytest.raises(ValueError):
+        pa.pi_attn_cache_store(k, k, *p.own, *p.own_exp, start=p.lens.long())
+    with pytest.raises(ValueError):
+        pa.pi_attn_cache_load(*p.own, *p.own_exp, -1)
+    with pytest.raises(ValueError):
+        pa.pi_attn_cache_load(*p.own, *p.own_exp, 4, k=k[:, :, :4], v=k[:, :, :4].transpose(0, 1).contiguous().transpose(0, 1))
+    with pytest.raises(pa.PiAttnError):   # rows that lie on one another
+        one = torch.zeros(1, 1, 1, D, device="cuda").expand(S, H, 5, D)
+        pa.pi_attn_cache_load(*p.own, *p.own_exp, 5, k=one, v=one.clone().as_strided(one.shape, one.stride()))
+    with pytest.raises(TypeError):
+        pa.pi_attn_cache_load(*p.own, *p.own_exp, 4, dtype=torch.float16)
+    torch.cuda.synchronize()
+    for x, y in zip(p.own, before):
+        assert torch.equal(x.view(torch.uint8), y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("what", ["key", "value"])
+@pytest.mark.parametrize("S,D", [(5, 64), (5, 128), (20, 64), (40, 128), (70, 64), (140, 128)])
+def test_not_finite_in_chunks(device, dtype, quant, what, S, D):
+    """The same where the prefix is taken in chunks: rows with NaN and infinities that only some windows hold; the other
+    sequences of the work-group keep their values."""
+    plen, cap, H, bad = (3000, 150, 2, 150) if D == 64 else (1600, 150, 2, 150)
+    k = plen - 100
+    lens = [(s * 29) % cap for s in range(S)]
+    p = Problem(dtype, quant, S, H, D, plen, cap, k, 0, lens)
+    assert pa.pi_attn_decode_workspace(dtype, S, H, D, plen, cap, k) > 0
+    want = p.expected()
+    x = p.shared[what == "value"]
+    for row, dim in ((bad, 33), (bad + 1, 33), (bad - 40, 5)):
+        if quant:
+            x.view(torch.uint8)[:, row, dim] = 0x7f if row == bad else 0xff
+        else:
+            x[:, row, dim] = float("nan") if row == bad else float("-inf")
+    out, lse = f64(p.run()), f64(p.lse)
+    for s, n in enumerate(lens):
+        lo = plen + n - k
+        if what == "key" and lo <= bad:   # the NaN logit, or one that is infinite of either sign
+            assert np.isnan(out[s]).all() and np.isnan(lse[s]).all()
+            continue
+        if what == "value":
+            for dim, rows in ((33, (bad, bad + 1)), (5, (bad - 40,))):
+                if lo <= max(rows):
+                    assert not np.isfinite(out[s, :, dim]).any()
+                    out[s, :, dim] = want.out[s, :, dim]
+        if what == "key" and lo <= bad + 1:
+            continue
+        assert np.all(np.abs(out[s] - want.out[s]) <= want.out_tol[s]), s
+        assert np.all(np.abs(lse[s] - want.lse[s]) <= want.lse_tol[s]), s
+
+
+def test_scale_past_the_largest_float(device):
+    """A value row whose scale byte makes its codes infinite, in windows of some sequences: the others keep their values."""
+    S, D, H, plen, cap, bad = 40, 128, 2, 1600, 150, 150
+    k = plen - 100
+    lens = [(s * 29) % cap for s in range(S)]
+    p = Problem(torch.bfloat16, True, S, H, D, plen, cap, k, 0, lens)
+    want = p.expected()
+    p.shared[1].view(torch.uint8)[:, bad] = 0x7e   # 448 * 2^(254 - 127)
+    p.shared_exp[1][:, bad] = 254
+    out = f64(p.run())
+    for s, n in enumerate(lens):
+        if plen + n - k <= bad:
+            assert not np.isfinite(out[s]).any()
+        else:
+            assert np.all(np.abs(out[s] - want.out[s]) <= want.out_tol[s]), s
