@@ -5,9 +5,12 @@
 // Of head h, sequence s at position t = plen + len_in[s] attends the prefix
 // rows max(0, t - k)..plen - 1: an end of the prefix, the same rows for every
 // sequence but for where they begin.  A work-group takes one chunk of the rows
-// of one head and a tile of sequences, and leaves for each of them the largest
+// of one head and a group of sequences, and leaves for each of them the largest
 // logit m of the chunk (log2 units), l = sum 2^(x - m) and the values weighted
-// alike, o; decode_cached.hip joins the chunks with the sequence's own rows.
+// alike, o; decode_cached.hip joins the chunks with the sequence's own rows.  A
+// chunk is every n-th tile of rows, so that whatever the windows leave is shared
+// by all work-groups, and the last tile comes first, which every window that
+// meets the prefix holds: the first loads wait for no length.
 //
 // Rows go from global memory straight into LDS as they are stored, through a
 // ring of stages: while a stage is worked on, the next ones are on their way,
@@ -15,7 +18,7 @@
 // row are XOR-swizzled by the row, each lane fetching the piece that belongs at
 // its place, so that no operand read below meets a bank twice.  e4m3 codes are
 // converted as they become operands: a key row's scale with its codes (exact),
-// a value row's in the weight (exact).  The four wavefronts of a work-group are
+// a value row's in the weight (exact).  The wavefronts of a work-group are
 // G groups of queries by RS shares of a stage's row blocks.  With one group
 // every wavefront has a ring of its own, and they wait for nobody until their
 // states are joined at the end.
@@ -34,6 +37,15 @@
 // row, for the sequences that do attend them.  (Added in their block, by
 // instructions other than the product's, they cost the product's loop 80
 // registers.)
+//
+// What bounds it, whole steps: HBM in bf16 (24 sequences of 16 heads behind 65536
+// rows, D = 128: 537 MB in 91 us, 5.9 TB/s; 64 of 32 behind 32768: 96 us) and in
+// e4m3 up to 32 sequences (32 of 32 heads behind 32768 rows: 271 MB in 58 us);
+// with 64 of e4m3 the softmax and the conversions, which overlap the loads only in
+// part (79 us; the loads alone 60, the arithmetic alone 61); from 128 the matrix
+// and the softmax instructions (bf16 127 us, e4m3 121); in float32 the products
+// (64 of 32 behind 8192: 97 us, 88 TFLOP/s).  Short of that the two launches, a
+// round trip each, and the parts, 17 MB written and read again at 64 of 32 heads.
 #include <algorithm>
 
 #include "bf16_rows.h"
@@ -830,7 +842,15 @@ auto with_shape(const CachedParams &p, bool bf16, F f) {
 
 }  // namespace
 
-constexpr int64_t kKeepPrefix = 64 << 20;
+// ONCE, by the bytes of the prefix rows that windows reach: the step of one layer
+// reads them once, and the other layers' come before the next.  With sixteen
+// layers in turn (more than the last-level cache together), kept and not: 16 MB
+// 17.5 and 16.2 us (bf16, D = 128, 16 sequences of 32 heads), 67 MB 29.4 and 26.4
+// (e4m3, 32 of 32), 134 MB 34.2 and 30.5, 537 MB 106 and 94.  With three, which
+// the cache holds up to 67 MB, the other way round there, 14.5 and 15.5, 24.5 and
+// 26.1.  Where work-groups of several tiles of sequences read the same rows, they
+// are kept.
+constexpr int64_t kKeepPrefix = 12 << 20;
 
 PrefixShape prefix_shape(const CachedParams &p, bool bf16) {
     return with_shape(p, bf16, [](auto s) {
