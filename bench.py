@@ -59,7 +59,7 @@ SMALLK_BWD_SOURCES = ("smallk_bwd_fused_bf16.hip", "smallk_bwd_bf16.hip", "small
                       "backward.hip", "pi_common.h", "kernels.h")
 BACKWARD_SOURCES = ("backward_bf16.hip", "backward_kv_bf16.hip", "bwd_tile.h", "bf16_rows.h", "backward.hip",
                     "pi_common.h", "kernels.h")
-DECODE_SOURCES = ("decode.hip", "pi_common.h", "kernels.h")
+DECODE_SOURCES = ("decode.hip", "decode_rows.h", "pi_common.h", "kernels.h")
 
 
 def csrc_digest(names):

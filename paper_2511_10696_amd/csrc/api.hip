@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/pi_attn.h"
+#include "cached.h"
 #include "kernels.h"
 #include "pi_common.h"
 #include "smallk.h"

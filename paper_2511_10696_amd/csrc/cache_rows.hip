@@ -17,9 +17,9 @@
 // What bounds them: HBM, by bytes moved (a bf16 row of 256 bytes becomes 129).
 // Large transfers leave the caches alone: what is read is not needed again, what
 // is written is more than they hold.
+#include "cached.h"
 #include "decode_rows.h"
 #include "e4m3.h"
-#include "kernels.h"
 #include "pi_common.h"
 
 namespace pi_attn {

@@ -22,9 +22,9 @@
 // leaving a part, and a last launch that joins them.
 #include <algorithm>
 
+#include "cached.h"
 #include "decode_rows.h"
 #include "e4m3.h"
-#include "kernels.h"
 #include "pi_common.h"
 
 namespace pi_attn {

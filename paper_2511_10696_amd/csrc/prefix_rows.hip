@@ -46,11 +46,9 @@
 // and the softmax instructions (bf16 127 us, e4m3 121); in float32 the products
 // (64 of 32 behind 8192: 97 us, 88 TFLOP/s).  Short of that the two launches, a
 // round trip each, and the parts, 17 MB written and read again at 64 of 32 heads.
-#include <algorithm>
-
 #include "bf16_rows.h"
+#include "cached.h"
 #include "e4m3.h"
-#include "kernels.h"
 #include "pi_common.h"
 
 namespace pi_attn {
