@@ -614,6 +614,14 @@ def pi_attn_decode_step(len_in, q_new, k_new, v_new, k_cache, v_cache, gate, k: 
     return out
 
 
+def _int32(name, x):
+    """An argument that the C call takes in 32 bits, which would be cut off silently."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit in 32 bits")
+    return x
+
+
 def _cache_checked(torch, k_cache, v_cache, k_exp, v_exp):
     """The sizes of a quantised cache."""
     if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
@@ -665,7 +673,7 @@ def pi_attn_cache_store(k, v, k_cache, v_cache, k_exp, v_exp, start=None, count=
     _per_sequence(torch, count, S, "count")
     with torch.cuda.device(k.device):
         st = library().pi_attn_cache_store(
-            _dtype_code(k.dtype), S, H, D, k.shape[2], cap, _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2),
+            _dtype_code(k.dtype), S, H, D, _int32("n", k.shape[2]), cap, _ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2),
             _ptr(start), _ptr(count), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp),
             _stream_handle(stream, k.device))
     _check(st, "pi_attn_cache_store")
@@ -685,7 +693,7 @@ def pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n: int, start=None, count
     _require_cuda(k_cache, v_cache, k_exp, v_exp, start, count, k, v)
     _same_device(k_cache, v_cache, k_exp, v_exp, start, count, k, v)
     S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
-    n = int(n)
+    n = _int32("n", n)
     if n < 0:
         raise ValueError("n must not be negative")
     if dtype is None:
@@ -711,7 +719,8 @@ def pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n: int, start=None, count
 def pi_attn_decode_workspace(dtype, S: int, H: int, D: int, plen: int, cap: int, k: int) -> int:
     """float32 elements of workspace that a step of pi_attn_decode_step_e4m3
     (plen = 0) or pi_attn_decode_step_prefix needs."""
-    n = int(library().pi_attn_decode_workspace(_dtype_code(dtype), int(S), int(H), int(D), int(plen), int(cap), int(k)))
+    sizes = [_int32(*x) for x in (("S", S), ("H", H), ("D", D), ("plen", plen), ("cap", cap), ("k", k))]
+    n = int(library().pi_attn_decode_workspace(_dtype_code(dtype), *sizes))
     if n < 0:
         raise PiAttnError(-1, "pi_attn_decode_workspace")
     return n
@@ -743,14 +752,12 @@ def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, ou
 
 def _workspace(torch, work, dtype, S, H, D, plen, cap, k, device, stream):
     """The caller's workspace (checked), a new one, or None where none is needed."""
-    need = int(library().pi_attn_decode_workspace(_dtype_code(dtype), S, H, D, plen, cap, int(k)))
+    need = int(library().pi_attn_decode_workspace(_dtype_code(dtype), S, H, D, plen, cap, _int32("k", k)))
     if work is None:
         if need <= 0:
             return None
-        work = torch.empty(need, dtype=torch.float32, device=device)
-        if stream is not None:   # let go at the return, it must not be handed out again before the step is done
-            work.record_stream(stream)
-        return work
+        with torch.cuda.device(device), torch.cuda.stream(stream):   # of the pool whose order the step follows
+            return torch.empty(need, dtype=torch.float32, device=device)
     if work.dtype != torch.float32 or not work.is_contiguous() or work.numel() < need:
         raise ValueError(f"work must be a contiguous float32 tensor of at least {need} elements")
     return work
@@ -777,7 +784,7 @@ def pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_ex
     work = _workspace(torch, work, q_new.dtype, S, H, D, 0, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_e4m3(
-            _dtype_code(q_new.dtype), S, H, D, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out), _ptr(q_new),
+            _dtype_code(q_new.dtype), S, H, D, cap, int(k), _int32("pi", pi), _ptr(len_in), _ptr(len_out), _ptr(q_new),
             _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(gate), gss, gsh,
             _scale(scale, D), float(logit_clamp), _ptr(out), _ptr(lse), _ptr(work),
             _stream_handle(stream, q_new.device))
@@ -835,7 +842,7 @@ def pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, 
     work = _workspace(torch, work, q_new.dtype, S, H, D, plen, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_prefix(
-            _dtype_code(q_new.dtype), S, H, D, plen, pcap, cap, int(k), int(pi), _ptr(len_in), _ptr(len_out),
+            _dtype_code(q_new.dtype), S, H, D, plen, pcap, cap, int(k), _int32("pi", pi), _ptr(len_in), _ptr(len_out),
             _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(k_prefix), _ptr(v_prefix), _ptr(k_prefix_exp),
             _ptr(v_prefix_exp), _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(gate), gss, gsh,
             _scale(scale, D), float(logit_clamp), _ptr(out), _ptr(lse), _ptr(work),
@@ -857,4 +864,4 @@ def _prefix_checked(k_prefix, v_prefix, dtype, H, D):
     pcap, rest = divmod(k_prefix.stride(0), D)
     if rest or pcap < plen:
         raise ValueError("the heads of k_prefix must lie whole rows apart, at least plen")
-    return plen, pcap
+    return plen, _int32("the rows between the heads of k_prefix", pcap)

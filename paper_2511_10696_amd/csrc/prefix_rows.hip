@@ -863,7 +863,8 @@ hipError_t launch_prefix(const CachedParams &p, bool bf16, hipStream_t stream) {
         const int n_qt = (p.d.S + S::QT - 1) / S::QT;
         const int64_t n = (int64_t)p.d.H * p.chunks * n_qt;
         const bool once = n_qt == 1 && 2 * (int64_t)p.d.H * p.near * S::R::RB > kKeepPrefix;
-        return launch_kernel(once ? prefix_kernel<S, true> : prefix_kernel<S, false>, dim3((unsigned)xcd_grid(n)), dim3(S::NT), stream, p, n_qt, (uint32_t)n);
+        return launch_kernel(once ? prefix_kernel<S, true> : prefix_kernel<S, false>, dim3((unsigned)xcd_grid(n)),
+                             dim3(S::NT), stream, p, n_qt, (uint32_t)n);
     });
 }
 

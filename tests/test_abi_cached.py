@@ -149,6 +149,15 @@ def test_workspace_size(lib):
         need(torch.float16, 1, 1, 64, 0, 10, 5)
 
 
+@pytest.mark.parametrize("at", range(6))
+def test_workspace_size_beyond_32_bits(lib, at):
+    """Sizes that the C call would take modulo 2^32 (2^32 + 4 for a window of 4)."""
+    sizes = [2, 3, 64, 100, 10, 5]
+    sizes[at] += 1 << 32
+    with pytest.raises(ValueError, match="32 bits"):
+        pa.pi_attn_decode_workspace(torch.bfloat16, *sizes)
+
+
 def test_binding_refuses_cpu_tensors(lib):
     kc = torch.zeros(1, 1, 8, 64).to(E4M3)
     e = torch.zeros(1, 1, 8, dtype=torch.uint8)

@@ -364,6 +364,42 @@ def test_same_bits_by_the_python_marshalling(device, quant):
     assert torch.equal(x, y) and torch.equal(a.lse, b.lse) and torch.equal(a.len_out, b.len_out)
 
 
+def test_workspace_of_a_given_stream(device, monkeypatch):
+    """Its memory comes from the pool of the stream that the step runs on: what another stream let go may still be in use
+    there."""
+    p = Problem(torch.bfloat16, True, 33, 40, 128, 700, 40, 600, 640, [s for s in range(33)])
+    side, empty, streams = torch.cuda.Stream(), torch.empty, []
+
+    def note(*a, **kw):
+        streams.append(torch.cuda.current_stream())
+        return empty(*a, **kw)
+
+    side.wait_stream(torch.cuda.current_stream())
+    monkeypatch.setattr(torch, "empty", note)
+    p.run(stream=side)
+    monkeypatch.undo()
+    assert streams == [side]
+    side.synchronize()
+
+
+def test_integers_beyond_32_bits(device):
+    """Refused, where their lowest 32 bits would be a valid window, period or count."""
+    p = Problem(torch.bfloat16, True, 2, 3, 64, 50, 20, 30, 0, [1, 2])
+    before = [x.view(torch.uint8).clone() for x in p.own]
+    big = 1 << 32
+    for k, pi in ((big + 30, 0), (30, big)):
+        with pytest.raises(ValueError, match="32 bits"):
+            pa.pi_attn_decode_step_prefix(p.lens, p.q, p.kn, p.vn, *p.shared, *p.own, p.gate, k, pi,
+                                          k_prefix_exp=p.shared_exp[0], v_prefix_exp=p.shared_exp[1], k_exp=p.own_exp[0],
+                                          v_exp=p.own_exp[1])
+        with pytest.raises(ValueError, match="32 bits"):
+            pa.pi_attn_decode_step_e4m3(p.lens, p.q, p.kn, p.vn, *p.own, *p.own_exp, p.gate, k, pi)
+    with pytest.raises(ValueError, match="32 bits"):
+        pa.pi_attn_cache_load(*p.own, *p.own_exp, big + 3)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y.view(torch.uint8)) for x, y in zip(before, p.own))
+
+
 def test_refusals(device):
     """What the binding refuses, each with one thing wrong."""
     S, H, D, plen, cap = 2, 3, 64, 50, 20
