@@ -306,8 +306,9 @@ int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int
  * one launch; otherwise its rows are taken in chunks, on the matrix cores, and
  * joined with the own rows by a second launch.
  * A length outside [0, cap): NaN for that sequence's outputs, its caches
- * untouched, len_out[s] = len_in[s].  bf16: the weights of the prefix rows
- * enter their value product as bf16.
+ * untouched, len_out[s] = len_in[s].  bf16: the weights of prefix rows
+ * that are taken in chunks enter their value product as two bf16 terms, off by
+ * 2^-15.
  * Errors: as pi_attn_decode_step, plus EINVAL for plen < 0, pcap < plen, some
  * but not all of the needed byte tables, a null or misaligned k_prefix,
  * v_prefix (plen > 0) or work that is needed; EUNSUPPORTED for S*H of 2^24 and

@@ -27,8 +27,12 @@
 // that a lane holds scores of one query and the probabilities are the B operand
 // of O^T = V^T P^T as they lie, the row order permuted alike in the V^T operand
 // (LDS transpose reads).  The running maximum is raised with every block that
-// has a larger logit, so a dominating row has weight 1 before it is rounded to
-// bf16; the sums are of the unrounded weights.
+// has a larger logit.  In bf16 a weight is the sum of two bf16 terms, two
+// products with each value operand, so that outputs are as near the definition
+// as with float32 weights, which a step has that reads its rows with vector
+// instructions.  One term, off by 2^-8, took 75 us where two take 85 (64
+// sequences of 32 heads behind 32768 e4m3 rows, D = 128), 122 and 144 (128
+// behind as many of bf16), 93 and 92 (24 of 16 behind 65536).
 //
 // Rows that begin before a sequence's window are masked in the blocks that
 // hold such rows.  A masked weight is 0, but 0 times an infinity or NaN is not:
@@ -99,6 +103,21 @@ __device__ inline bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight weights p as sums of two bf16 terms: hi, p without its low 16 bits, and lo, the rest, which is below 2^-7 p and is
+// rounded by at most 2^-8 of itself: 2^-15 p.  The rest of p (1 + 2^-23) is taken, which is not 0 where p is not, so that
+// an infinite value has two products of one sign and stays infinite.
+__device__ inline void split8(const float *p, bf16x8 &hi, bf16x8 &lo) {
+    unsigned h[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const unsigned a = __float_as_uint(p[e]), b = __float_as_uint(p[e + 1]);
+        h[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        lo[e] = (__bf16)__builtin_fmaf(p[e], 1.0f + 0x1p-23f, -__uint_as_float(a & 0xffff0000u));
+        lo[e + 1] = (__bf16)__builtin_fmaf(p[e + 1], 1.0f + 0x1p-23f, -__uint_as_float(b & 0xffff0000u));
+    }
+    hi = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
 }
 
 // ---- one block of rows with a wavefront's queries -------------------------------
@@ -203,11 +222,9 @@ struct Mma<__bf16, ST, D, NG> {
     __device__ void values(const float (&p)[NG][NS]) {
 #pragma unroll
         for (int cc = 0; cc < 2; ++cc) {
-            bf16x8 pb[NG];
+            bf16x8 hi[NG], lo[NG];
 #pragma unroll
-            for (int n = 0; n < NG; ++n)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pb[n][e] = (__bf16)p[n][8 * cc + e];
+            for (int n = 0; n < NG; ++n) split8(&p[n][8 * cc], hi[n], lo[n]);
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) {
                 bf16x8 vf;
@@ -218,8 +235,10 @@ struct Mma<__bf16, ST, D, NG> {
                     vf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
 #pragma unroll
-                for (int n = 0; n < NG; ++n)
-                    o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[n], o[n][b], 0, 0, 0);
+                for (int n = 0; n < NG; ++n) {
+                    o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi[n], o[n][b], 0, 0, 0);
+                    o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, lo[n], o[n][b], 0, 0, 0);
+                }
             }
         }
     }
