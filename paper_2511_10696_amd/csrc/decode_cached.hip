@@ -201,7 +201,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
             for (int e = 0; e < EPL; ++e) part += qf[e] * kf[e];
             part = row_sum<LPR>(part);
             if constexpr (Q) part *= e4m3_scale(byte);
-            if constexpr (CLAMP) return fminf(fmaxf(part * d.scale + bias, -d.clamp), d.clamp) * kLog2e;
+            if constexpr (CLAMP) return clamped_logit(part * d.scale + bias, d.clamp) * kLog2e;
             return part * c2 + bias * kLog2e;
         };
 

@@ -652,7 +652,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
             for (int n = 0; n < NG; ++n)
 #pragma unroll
                 for (int i = 0; i < M::NS; ++i)
-                    sc[n][i] = fminf(fmaxf(sc[n][i] * d.scale + bias[n], -d.clamp), d.clamp) * kLog2e;
+                    sc[n][i] = clamped_logit(sc[n][i] * d.scale + bias[n], d.clamp) * kLog2e;
         }
         if (masked || j0 + KB > plen) {
 #pragma unroll
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
                 for (int n = 0; n < NG; ++n) {
                     float sc = query_sum<QB>(mm.dot(n, kr, g));
                     if constexpr (Q) sc *= e4m3_scale(p.k_prefix_exp[head + j]);
-                    if (clamped) sc = fminf(fmaxf(sc * d.scale + bias[n], -d.clamp), d.clamp) * kLog2e;
+                    if (clamped) sc = clamped_logit(sc * d.scale + bias[n], d.clamp) * kLog2e;
                     const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(sc, c2, -m[n]));
                     const bool in = j >= lo[n];
 #pragma unroll
