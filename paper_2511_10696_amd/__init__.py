@@ -24,6 +24,10 @@ bidirectional mode, window |j - t| <= k and partners t -/+ pi):
     pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k, pi)
 Quantised caches are torch.float8_e4m3fn codes [S,H,cap,D] with a torch.uint8
 scale byte for each row [S,H,cap].
+
+A call runs on the current stream, or on the given one.  What it allocates then
+belongs to that stream, as if it had been the current one: other streams wait for
+it before they use a result, and record_stream() it if they outlive its tensor.
 """
 from __future__ import annotations
 
@@ -166,6 +170,12 @@ def _stream_handle(stream, device):
     if stream is None:
         stream = torch.cuda.current_stream(device)
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _on(stream):
+    """What a call on a given stream allocates belongs to that stream's pool:
+    memory that the current one let go may still be in use there."""
+    return _torch().cuda.stream(stream)
 
 
 def _ptr(t):
@@ -698,10 +708,11 @@ def pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n: int, start=None, count
         raise ValueError("n must not be negative")
     if dtype is None:
         dtype = torch.bfloat16 if k is None and v is None else (v if k is None else k).dtype
-    if k is None:
-        k = torch.empty((S, H, n, D), dtype=dtype, device=k_cache.device) if v is None else torch.empty_like(v)
-    if v is None:
-        v = torch.empty_like(k)
+    with _on(stream):
+        if k is None:
+            k = torch.empty((S, H, n, D), dtype=dtype, device=k_cache.device) if v is None else torch.empty_like(v)
+        if v is None:
+            v = torch.empty_like(k)
     for t in (k, v):
         if tuple(t.shape) != (S, H, n, D) or t.dtype != dtype or t.stride() != k.stride() or t.stride(3) != 1:
             raise ValueError(f"k and v must be {dtype} [{S}, {H}, {n}, {D}] tensors that share strides, with a "
@@ -726,7 +737,7 @@ def pi_attn_decode_workspace(dtype, S: int, H: int, D: int, plen: int, cap: int,
     return n
 
 
-def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse):
+def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse, stream):
     """The arguments that the cached decode steps share; the output and the gate's strides."""
     for name, t in (("q_new", q_new), ("k_new", k_new), ("v_new", v_new)):
         if tuple(t.shape) != (S, H, D) or not t.is_contiguous() or t.dtype != q_new.dtype:
@@ -742,7 +753,8 @@ def _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, ou
     else:
         raise ValueError("decode gate must be [H] or [S, H]")
     if out is None:
-        out = torch.empty_like(q_new)
+        with _on(stream):
+            out = torch.empty_like(q_new)
     if tuple(out.shape) != (S, H, D) or out.dtype != q_new.dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous [S, H, D] tensor of q_new's dtype")
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (S, H) or not lse.is_contiguous()):
@@ -756,7 +768,7 @@ def _workspace(torch, work, dtype, S, H, D, plen, cap, k, device, stream):
     if work is None:
         if need <= 0:
             return None
-        with torch.cuda.device(device), torch.cuda.stream(stream):   # of the pool whose order the step follows
+        with torch.cuda.device(device), _on(stream):
             return torch.empty(need, dtype=torch.float32, device=device)
     if work.dtype != torch.float32 or not work.is_contiguous() or work.numel() < need:
         raise ValueError(f"work must be a contiguous float32 tensor of at least {need} elements")
@@ -780,7 +792,7 @@ def pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_ex
     _require_cuda(*ts)
     _same_device(*ts)
     S, H, cap, D = _cache_checked(torch, k_cache, v_cache, k_exp, v_exp)
-    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
+    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse, stream)
     work = _workspace(torch, work, q_new.dtype, S, H, D, 0, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_e4m3(
@@ -838,7 +850,7 @@ def pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, 
             if t.dtype != torch.uint8 or tuple(t.shape) != (H, plen) or (
                     plen > 1 and t.stride(1) != 1 or H > 1 and plen > 0 and t.stride(0) != pcap):
                 raise ValueError(f"{name} must be a uint8 [H, plen] tensor that lies as the rows of k_prefix do")
-    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse)
+    out, (gss, gsh) = _step_checked(torch, len_in, q_new, k_new, v_new, S, H, D, gate, len_out, out, lse, stream)
     work = _workspace(torch, work, q_new.dtype, S, H, D, plen, cap, k, q_new.device, stream)
     with torch.cuda.device(q_new.device):
         st = library().pi_attn_decode_step_prefix(
