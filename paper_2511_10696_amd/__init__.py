@@ -31,6 +31,7 @@ it before they use a result, and record_stream() it if they outlive its tensor.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import threading
@@ -175,7 +176,7 @@ def _stream_handle(stream, device):
 def _on(stream):
     """What a call on a given stream allocates belongs to that stream's pool:
     memory that the current one let go may still be in use there."""
-    return _torch().cuda.stream(stream)
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
 
 
 def _ptr(t):
@@ -197,10 +198,11 @@ def _require_cuda(*ts):
             raise RuntimeError("pi_attn tensors must be on the GPU (no CPU path exists)")
 
 
-def _out_f32(torch, given, shape, device, name):
+def _out_f32(torch, given, shape, device, name, stream):
     """A caller's float32 output buffer (checked: contiguous, the shape), or a new one."""
     if given is None:
-        return torch.empty(shape, dtype=torch.float32, device=device)
+        with _on(stream):
+            return torch.empty(shape, dtype=torch.float32, device=device)
     _require_cuda(given)
     if given.dtype != torch.float32 or tuple(given.shape) != tuple(shape) or not given.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)}")
@@ -226,7 +228,8 @@ def pi_attn_index_set(n: int, k: int, pi: int, out=None, device=None, stream=Non
     if m < 0:
         raise PiAttnError(-1, "pi_attn_index_set")
     if out is None:
-        out = torch.empty((n, m), dtype=torch.int32, device=device or "cuda")
+        with _on(stream):
+            out = torch.empty((n, m), dtype=torch.int32, device=device or "cuda")
     _require_cuda(out)
     if out.dtype != torch.int32 or tuple(out.shape) != (n, m) or not out.is_contiguous():
         raise ValueError(f"out must be a contiguous int32 tensor of shape {(n, m)}")
@@ -269,11 +272,13 @@ def pi_attn_forward(q, k, v, gate, k_window: int, pi: int, scale: float | None =
     else:
         raise ValueError(f"gate must be [H] or [B, H, N], got {tuple(gate.shape)}")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        with _on(stream):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("out must match q's shape and dtype with a contiguous last dimension")
     if return_lse and lse is None:
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, H, N)
                             or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [B, H, N] tensor")
@@ -319,11 +324,13 @@ def pi_attn_forward_shard(q, k, v, gate, k_window: int, pi: int, nseq: int, qpos
     else:
         raise ValueError(f"gate must be [H] or [B, H, nq], got {tuple(gate.shape)}")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        with _on(stream):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("out must match q's shape and dtype with a contiguous last dimension")
     if return_lse and lse is None:
-        lse = torch.empty((B, H, nq), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            lse = torch.empty((B, H, nq), dtype=torch.float32, device=q.device)
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, H, nq)
                             or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [B, H, nq] tensor")
@@ -363,9 +370,9 @@ def pi_attn_backward_shard_q(q, k, v, gate, k_window: int, pi: int, nseq: int, q
     if k.shape != v.shape or k.stride() != v.stride() or k.shape[:2] != q.shape[:2] or k.shape[3] != D:
         raise ValueError("k, v [B, H, nkv, D] with shared strides")
     g = _shard_gate(torch, gate, B, H, nq)
-    dq = _out_f32(torch, dq, (B, H, nq, D), q.device, "dq")
-    dg = _out_f32(torch, dgate, (B, H, nq), q.device, "dgate")
-    rt = _out_f32(torch, rowterm, (B, H, nq), q.device, "rowterm")
+    dq = _out_f32(torch, dq, (B, H, nq, D), q.device, "dq", stream)
+    dg = _out_f32(torch, dgate, (B, H, nq), q.device, "dgate", stream)
+    rt = _out_f32(torch, rowterm, (B, H, nq), q.device, "rowterm", stream)
     scale = _scale(scale, D)
     st = library().pi_attn_backward_shard_q(
         _dtype_code(q.dtype), B, H, D, int(k_window), int(pi), int(bool(causal)), int(nseq), int(qpos0), nq,
@@ -397,8 +404,8 @@ def pi_attn_backward_shard_kv(q, k, v, gate, k_window: int, pi: int, nseq: int, 
         if x.dtype != torch.float32 or tuple(x.shape) != (B, H, nqh) or not x.is_contiguous():
             raise ValueError(f"{name} must be a contiguous float32 [B, H, nqh] tensor")
     g = _shard_gate(torch, gate, B, H, nqh)
-    dk = _out_f32(torch, dk, (B, H, nk, D), k.device, "dk")
-    dv = _out_f32(torch, dv, (B, H, nk, D), k.device, "dv")
+    dk = _out_f32(torch, dk, (B, H, nk, D), k.device, "dk", stream)
+    dv = _out_f32(torch, dv, (B, H, nk, D), k.device, "dv", stream)
     scale = _scale(scale, D)
     st = library().pi_attn_backward_shard_kv(
         _dtype_code(k.dtype), B, H, D, int(k_window), int(pi), int(bool(causal)), int(nseq), int(kpos0), nk,
@@ -445,15 +452,18 @@ def pi_attn_forward_gated(q, k, v, u, w2, b2, k_window: int, pi: int, scale: flo
     if b2 is not None and (b2.dtype != torch.float32 or tuple(b2.shape) != (H,) or not b2.is_contiguous()):
         raise ValueError("b2 must be a contiguous float32 [H] tensor or None")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        with _on(stream):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("out must match q's shape and dtype with a contiguous last dimension")
     if gate_out is None:
-        gate_out = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            gate_out = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
     if gate_out.dtype != torch.float32 or tuple(gate_out.shape) != (B, H, N) or not gate_out.is_contiguous():
         raise ValueError("gate_out must be a contiguous float32 [B, H, N] tensor")
     if return_lse and lse is None:
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            lse = torch.empty((B, H, N), dtype=torch.float32, device=q.device)
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, H, N)
                             or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [B, H, N] tensor")
@@ -494,8 +504,9 @@ def pi_attn_backward(q, k, v, gate, k_window: int, pi: int, out, lse, dout, scal
     if k.dtype != q.dtype or v.dtype != q.dtype or dout.dtype != q.dtype or out.dtype != q.dtype:
         raise TypeError("q, k, v, out, dout must share one dtype")
     if out.stride() != dout.stride():
-        dout = dout.contiguous()
-        out = out.contiguous()
+        with _on(stream):
+            dout = dout.contiguous()
+            out = out.contiguous()
     if k.stride() != q.stride() or v.stride() != q.stride():
         raise ValueError("q, k, v must share strides (use .contiguous())")
     if q.stride(3) != 1 or dout.stride(3) != 1:
@@ -512,9 +523,10 @@ def pi_attn_backward(q, k, v, gate, k_window: int, pi: int, out, lse, dout, scal
     if lse.dtype != torch.float32 or tuple(lse.shape) != (B, H, N) or not lse.is_contiguous():
         raise ValueError("lse must be the contiguous float32 [B, H, N] lse of the forward")
     f32 = dict(dtype=torch.float32, device=q.device)
-    dq, dk, dv = (_out_f32(torch, x, (B, H, N, D), q.device, n) for x, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")))
-    dg = _out_f32(torch, dgate, (B, H, N), q.device, "dgate")
-    rowterm = _out_f32(torch, rowterm, (B, H, N), q.device, "rowterm")
+    dq, dk, dv = (_out_f32(torch, x, (B, H, N, D), q.device, n, stream)
+                  for x, n in ((dq, "dq"), (dk, "dk"), (dv, "dv")))
+    dg = _out_f32(torch, dgate, (B, H, N), q.device, "dgate", stream)
+    rowterm = _out_f32(torch, rowterm, (B, H, N), q.device, "rowterm", stream)
     scale = _scale(scale, D)
     st = library().pi_attn_backward(
         _dtype_code(q.dtype), B, H, N, D, int(k_window), int(pi), int(bool(causal)),
@@ -524,7 +536,8 @@ def pi_attn_backward(q, k, v, gate, k_window: int, pi: int, out, lse, dout, scal
         _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg), _ptr(rowterm), _stream_handle(stream, q.device))
     _check(st, "pi_attn_backward")
     if tuple(gate.shape) == (H,) and not gate_grad_per_query:
-        dgh = torch.empty((H,), **f32)
+        with _on(stream):
+            dgh = torch.empty((H,), **f32)
         _check(library().pi_attn_gate_grad_per_head(B, H, N, _ptr(dg), _ptr(dgh), _stream_handle(stream, q.device)),
                "pi_attn_gate_grad_per_head")
         dg = dgh
@@ -607,7 +620,8 @@ def pi_attn_decode_step(len_in, q_new, k_new, v_new, k_cache, v_cache, gate, k: 
     else:
         raise ValueError("decode gate must be [H] or [S, H]")
     if out is None:
-        out = torch.empty_like(q_new)
+        with _on(stream):
+            out = torch.empty_like(q_new)
     if tuple(out.shape) != (S, H, D) or out.dtype != k_cache.dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous [S, H, D] tensor of the cache dtype")
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (S, H) or not lse.is_contiguous()):

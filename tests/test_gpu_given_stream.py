@@ -47,3 +47,45 @@ def test_load(device, given):
     for x, y, name in zip(got, want, "kv"):
         assert x is mine[name] if name in mine else pool_of(x) == side.cuda_stream
         assert torch.equal(x.nan_to_num(9), y.nan_to_num(9))
+
+
+def same(call, n_out):
+    """call(stream=None) and on a given stream: the same bits, the latter's from the stream's pool."""
+    want = call()
+    side = given_stream()
+    got = call(stream=side)
+    side.synchronize()
+    want, got = (x if isinstance(x, tuple) else (x,) for x in (want, got))
+    assert len(got) == len(want) == n_out
+    for x, y in zip(got, want):
+        assert pool_of(x) == side.cuda_stream
+        assert torch.equal(x, y)
+
+
+def test_full_sequence_calls(device):
+    B, H, N, D, k, pi = 1, 2, 200, 64, 40, 50
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    q, kk, v, dout = (rnd(B, H, N, D) for _ in range(4))
+    gate = torch.rand(H, generator=g, device="cuda")
+    u, w2 = rnd(B, N, 32), rnd(H, 32)
+    same(lambda **kw: pa.pi_attn_index_set(30, 4, 7, **kw), 1)
+    same(lambda **kw: pa.pi_attn_forward(q, kk, v, gate, k, pi, return_lse=True, **kw), 2)
+    same(lambda **kw: pa.pi_attn_forward_gated(q, kk, v, u, w2, None, k, pi, return_lse=True, **kw), 3)
+    out, lse = pa.pi_attn_forward(q, kk, v, gate, k, pi, return_lse=True)
+    for d in (dout, dout.transpose(1, 2).contiguous().transpose(1, 2)):   # the latter is copied first
+        same(lambda **kw: pa.pi_attn_backward(q, kk, v, gate, k, pi, out, lse, d, **kw), 4)
+    same(lambda **kw: pa.pi_attn_forward_shard(q[:, :, 80:], kk, v, gate, k, pi, N, 80, 0, return_lse=True, **kw), 2)
+    same(lambda **kw: pa.pi_attn_backward_shard_q(q, kk, v, gate, k, pi, N, 0, 0, out, lse, dout, **kw), 3)
+    rt = pa.pi_attn_backward_shard_q(q, kk, v, gate, k, pi, N, 0, 0, out, lse, dout)[2]
+    same(lambda **kw: pa.pi_attn_backward_shard_kv(q, kk, v, gate, k, pi, N, 0, 0, lse, rt, dout, **kw), 2)
+
+
+def test_decode_step(device):
+    S, H, D, cap = 3, 2, 64, 50
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(S, H, D, generator=g, device="cuda")
+    kc, vc = (torch.randn(S, H, cap, D, generator=g, device="cuda") for _ in range(2))
+    lens = torch.tensor([0, 20, 49], dtype=torch.int32, device="cuda")
+    gate = torch.zeros(H, device="cuda")
+    same(lambda **kw: pa.pi_attn_decode_step(lens, x, x, x, kc, vc, gate, 10, 15, **kw), 1)
