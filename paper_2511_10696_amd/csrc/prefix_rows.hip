@@ -373,6 +373,21 @@ struct Mma<float, ST, D, NG> {
     }
 };
 
+// A weight 2^(s c - m) of a score s, m the largest of the rounded s c.  The product is rounded with the difference, which
+// costs nothing and keeps its last bits; but then the largest score's weight is 2^r, r the rounding of m.  WIDE, once some
+// |m| has passed 2^22 (r up to 1/4; at 2^32 it would be 256): rounded first, as m is, so that the largest weight is 1.
+constexpr float kWide = 0x1p22f;
+
+template <bool WIDE>
+__device__ inline float weight(float s, float c, float m) {
+    if constexpr (WIDE) {
+#pragma clang fp contract(off)
+        const float x = s * c;
+        return __builtin_amdgcn_exp2f(x - m);
+    }
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -m));
+}
+
 // Maximum and sum over the lanes of a query.
 __device__ inline float other_row(float x) {   // of the neighbouring 16 lanes
     const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -606,6 +621,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
     // Zeros for the values of a block that are not finite.  Wavefronts that share
     // the block may all do so: each has written its zeros before it reads.
     bool cleaned = false;   // wave-uniform
+    bool wide = false;      // and so
     auto clean = [&](unsigned char *vb, unsigned *vbytes) {
         cleaned = true;
         if (!S::OWN) s_cleaned = 1;
@@ -674,23 +690,30 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
             raised |= mx[n] > m[n];
         }
         if (__builtin_amdgcn_ballot_w64(raised)) {
+            bool large = false;
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
+                large |= mx[n] > m[n] && fabsf(mx[n]) > kWide;
                 const float m_new = fmaxf(m[n], mx[n]);
                 const float alpha = mx[n] > m[n] ? __builtin_amdgcn_exp2f(m[n] - m_new) : 1.0f;
                 m[n] = m_new;
                 l[n] *= alpha;
                 mm.scale(n, alpha);
             }
+            wide |= __builtin_amdgcn_ballot_w64(large) != 0;
         }
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
             const float m_use = m[n] == -INFINITY ? 0.0f : m[n];
+            if (wide) {
 #pragma unroll
-            for (int i = 0; i < M::NS; ++i) {
-                sc[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i], c2, -m_use));
-                l[n] += sc[n][i];
+                for (int i = 0; i < M::NS; ++i) sc[n][i] = weight<true>(sc[n][i], c2, m_use);
+            } else {
+#pragma unroll
+                for (int i = 0; i < M::NS; ++i) sc[n][i] = weight<false>(sc[n][i], c2, m_use);
             }
+#pragma unroll
+            for (int i = 0; i < M::NS; ++i) l[n] += sc[n][i];
         }
         if constexpr (Q) {
 #pragma unroll
@@ -762,7 +785,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
                     float sc = query_sum<QB>(mm.dot(n, kr, g));
                     if constexpr (Q) sc *= e4m3_scale(p.k_prefix_exp[head + j]);
                     if (clamped) sc = clamped_logit(sc * d.scale + bias[n], d.clamp) * kLog2e;
-                    const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(sc, c2, -m[n]));
+                    const float pr = wide ? weight<true>(sc, c2, m[n]) : weight<false>(sc, c2, m[n]);
                     const bool in = j >= lo[n];
 #pragma unroll
                     for (int z = 0; z < M::NO; ++z) {
