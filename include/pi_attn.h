@@ -302,9 +302,10 @@ int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int
  *   work         as pi_attn_decode_step_e4m3, for plen.
  * The prefix must not overlap rows that the step writes.  Which kernels run
  * depends on the sizes alone, the sums are taken in a fixed order: the same call
- * gives the same bits.  A small prefix is read by every sequence for itself, in
- * one launch; otherwise its rows are taken in chunks, on the matrix cores, and
- * joined with the own rows by a second launch.
+ * gives the same bits.  A small prefix is read by every sequence for itself, with
+ * its own rows; otherwise its rows are taken in chunks, on the matrix cores, and
+ * joined with the own rows by a second launch.  Long own windows of a few (s, h)
+ * are split as in pi_attn_decode_step_e4m3.
  * A length outside [0, cap): NaN for that sequence's outputs, its caches
  * untouched, len_out[s] = len_in[s].  bf16: the weights of prefix rows
  * that are taken in chunks enter their value product as two bf16 terms, off by

@@ -20,7 +20,7 @@
 //
 // Few (s, h) with long windows: a work-group per range of own rows, each
 // leaving a part, and a last launch that joins them.  Short prefixes: read with
-// the own rows, in one launch.
+// the own rows, in the same launch.
 //
 // What bounds it: HBM with many long windows (64 sequences of 32 heads, D = 128,
 // k = 512, e4m3: 274 MB in 45 us, 6.1 TB/s; 90 from bf16 caches), one launch and
@@ -80,14 +80,16 @@ __device__ inline uint4 quantise16(const float (&x)[16], unsigned &byte) {
 
 // What a launch does of a step: all of it, where no prefix row is in a window
 // (ALONE), where they were taken in parts (WHOLE) or are read here, by each
-// sequence for itself (DIRECT); one range of own rows (RANGE: a part), or the
-// join of the parts (JOIN).
-enum { ALONE, WHOLE, DIRECT, RANGE, JOIN };
+// sequence for itself (DIRECT); one range of own rows (RANGE: a part), or of
+// prefix and own rows (DIRECT_RANGE); or the join of the parts (JOIN).
+enum { ALONE, WHOLE, DIRECT, RANGE, DIRECT_RANGE, JOIN };
 
 template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams p) {
     using R = Row<ST, D>;
     constexpr bool Q = kQuantised<ST>;
+    constexpr bool PART = MODE == RANGE || MODE == DIRECT_RANGE;
+    constexpr bool BOTH = MODE == DIRECT || MODE == DIRECT_RANGE;   // window rows in either table
     constexpr int LPR = R::LPR, RPI = R::RPI, EPL = R::EPL;
     constexpr int RPC = RPI * CH;   // rows per chunk
 
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     __shared__ float s_acc[WAVES][D];
 
     const DecodeParams &d = p.d;
-    const DivMod range_of = divmod(blockIdx.x, MODE == RANGE ? p.own_parts : 1);
+    const DivMod range_of = divmod(blockIdx.x, PART ? p.own_parts : 1);
     const int64_t sh = range_of.quot;
     const int range = (int)range_of.rem;
     const DivMod head_of = divmod(range_of.quot, d.H);
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
     const FusionBias fb = fusion_bias(d.gate[s * d.gss + h * d.gsh], CLAMP);
 
     if (n < 0 || n >= d.cap) {
-        if (MODE == RANGE) return;
+        if (PART) return;
         for (int i = tid; i < D; i += 64 * WAVES) out[i] = (T)NAN;
         if (tid == 0) {
             if (d.lse) d.lse[sh] = NAN;
@@ -156,15 +158,15 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
         wide_f32<T, EPL>(qw, qf);
         const float c2 = d.scale * kLog2e;
 
-        // window rows first + [0, nwin): own rows, or (DIRECT) positions
-        const int first = MODE == DIRECT ? lo : max(lo - p.plen, 0);
-        const int nwin = (MODE == DIRECT ? t : n) - first;
+        // window rows first + [0, nwin): own rows, or (BOTH) positions
+        const int first = BOTH ? lo : max(lo - p.plen, 0);
+        const int nwin = (BOTH ? t : n) - first;
         const int64_t shared = h * p.pcap;
         const uint8_t *kp = (const uint8_t *)p.k_prefix + (shared * D + sub * EPL) * sizeof(ST);
         const uint8_t *vp = (const uint8_t *)p.v_prefix + (shared * D + sub * EPL) * sizeof(ST);
         const int all = (nwin + RPC - 1) / RPC;
         // this launch's chunks
-        const int per = MODE == RANGE ? (all + p.own_parts - 1) / p.own_parts : all;
+        const int per = PART ? (all + p.own_parts - 1) / p.own_parts : all;
         const int chunk0 = min(range * per, all), nchunks = min(per, all - chunk0);
 
         uint4 kr[CH], vr[CH];
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
                 int64_t row = first + min(ch * RPC + c * RPI + rg, nwin - 1);
                 const uint8_t *ka = kc, *va = vc;
                 const uint8_t *kea = p.k_exp + head, *vea = p.v_exp + head;
-                if constexpr (MODE == DIRECT) {
+                if constexpr (BOTH) {
                     const bool own = row >= p.plen;
                     row = own ? row - p.plen : row;
                     ka = own ? ka : kp;
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_cached_kernel(CachedParams 
             L += s_l[x] * f;
             o += s_acc[x][i] * f;
         }
-        if (MODE == RANGE) {
+        if (PART) {
             const int64_t at = (int64_t)(p.chunks + range) * n_sh + sh;
             p.part_o[at * D + i] = o;
             if (i == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(M, L);
@@ -378,9 +380,9 @@ constexpr int64_t kKeepBytes = 12 << 20;
 template <typename T, typename ST, int D, bool CLAMP, int MODE, int WAVES, int CH>
 hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
-    constexpr bool kMany = MODE != DIRECT && MODE != JOIN;   // window rows of its own, and many
+    constexpr bool kMany = MODE != DIRECT && MODE != DIRECT_RANGE && MODE != JOIN;   // window rows of its own, and many
     const bool once = kMany && 2 * n * std::min(p.d.k, p.d.cap) * D * (int64_t)sizeof(ST) > kKeepBytes;
-    const int64_t groups = n * (MODE == RANGE ? p.own_parts : 1);
+    const int64_t groups = n * (MODE == RANGE || MODE == DIRECT_RANGE ? p.own_parts : 1);
     return launch_kernel(once ? decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, kMany>
                               : decode_cached_kernel<T, ST, D, CLAMP, MODE, WAVES, CH, false>,
                          dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
@@ -401,13 +403,14 @@ hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
     const int rows = std::min(p.d.k, p.d.cap) + (p.direct ? p.near : 0);
     const int loads = (rows + Row<ST, D>::RPI - 1) / Row<ST, D>::RPI;
     const bool many = n >= 2048;
+    if (p.own_parts) {
+        const hipError_t e = p.direct ? launch_n<T, ST, D, CLAMP, DIRECT_RANGE, 4, 4>(p, stream)
+                                      : launch_n<T, ST, D, CLAMP, RANGE, 4, 4>(p, stream);
+        return e != hipSuccess ? e : launch_n<T, ST, D, CLAMP, JOIN, 4, 4>(p, stream);
+    }
     if (p.direct) {
         return loads > 32 ? launch_n<T, ST, D, CLAMP, DIRECT, 8, 4>(p, stream)
                           : launch_n<T, ST, D, CLAMP, DIRECT, 4, 4>(p, stream);
-    }
-    if (p.own_parts) {
-        const hipError_t e = launch_n<T, ST, D, CLAMP, RANGE, 4, 4>(p, stream);
-        return e != hipSuccess ? e : launch_n<T, ST, D, CLAMP, JOIN, 4, 4>(p, stream);
     }
     if (p.chunks) {
         if (loads <= 8) return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
@@ -430,7 +433,7 @@ hipError_t launch_t(const CachedParams &p, hipStream_t stream) {
 
 }  // namespace
 
-// Whether the sequences read the prefix's rows for themselves, in one launch: as
+// Whether the sequences read the prefix's rows for themselves, with their own: as
 // long as one (s, h) has a chain of few loads, and all of them together little
 // more than the launch that is saved.  us, by chunks and so: bf16 D = 64, 64
 // (s, h) 1024 rows 8.7 and 7.3, 2048 rows 8.8 and 10.5; D = 128, 128 (s, h) 512
@@ -448,7 +451,10 @@ bool read_directly(const CachedParams &p, int element_bytes) {
 // work-groups, of 64 KB at least.  us, whole and split, e4m3, D = 128: 32 (s, h)
 // of 1600 rows 13.5 and 11.1, of 16384 rows 99.4 and 27.8; 64 of 2048 17.0 and
 // 13.1, 128 of 2048 18.3 and 18.2; 256 of 2048 24.5 and 28.2, of 8192 80.9 and
-// 85.0; 1024 and 2048 work-groups the same but for 256 (s, h) and one.
+// 85.0; 1024 and 2048 work-groups the same but for 256 (s, h) and one.  Behind 200
+// prefix rows that are read with them: 32 (s, h) of 16384 rows 112.8 and 32.7, of
+// 1700 15.6 and 11.1, 128 of 1600 15.2 and 15.7, of 4000 35.6 and 31.0; bf16 32 of
+// 8000 81.6 and 29.7, of 1000 12.8 and 10.0.
 int own_parts(const CachedParams &p, int element_bytes) {
     const int64_t n = (int64_t)p.d.S * p.d.H, own = std::min(p.d.k, p.d.cap - 1);
     const int64_t bytes = 2 * own * p.d.D * element_bytes;   // keys and values of an (s, h)
@@ -485,7 +491,7 @@ hipError_t launch_decode_cached(const CachedParams &planned, bool bf16, hipStrea
         p.direct = true;
         p.chunks = 0;
     }
-    p.own_parts = p.direct ? 0 : own_parts(p, p.k_exp ? 1 : bf16 ? 2 : 4);
+    p.own_parts = own_parts(p, p.k_exp ? 1 : bf16 ? 2 : 4);
     if (p.chunks) {
         const PrefixShape shape = prefix_shape(p, bf16);
         const int64_t side = (int64_t)p.d.H * ((p.d.S + shape.queries - 1) / shape.queries);
