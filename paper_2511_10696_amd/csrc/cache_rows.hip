@@ -19,6 +19,8 @@
 // read and written, a plain copy 4.8), 16 sequences of 2000 read in 131.
 // Large transfers leave the caches alone: what is read is not needed again, what
 // is written is more than they hold.
+#include <algorithm>
+
 #include "cached.h"
 #include "decode_rows.h"
 #include "e4m3.h"
@@ -39,14 +41,15 @@ struct Place {
 template <int RPI, int U, bool RUNS>
 __device__ inline Place place(int u, int rg, const CacheRowsParams &p) {
     const int w = threadIdx.x >> 6;
+    const uint32_t group = p.first_group + blockIdx.x;
     if constexpr (RUNS) {
-        const DivMod inner = divmod(blockIdx.x, p.heads_first ? p.H : p.runs);
+        const DivMod inner = divmod(group, p.heads_first ? p.H : p.runs);
         const DivMod outer = divmod(inner.quot, p.heads_first ? p.runs : p.H);
         const int h = (int)(p.heads_first ? inner.rem : outer.rem), run = (int)(p.heads_first ? outer.rem : inner.rem);
         const int i = run * (WAVES * U * RPI) + (w * U + u) * RPI + rg;
         return Place{(int)outer.quot, h, i < p.n ? i : -1};
     } else {
-        const uint32_t r = (blockIdx.x * WAVES + w) * (U * RPI) + u * RPI + rg;
+        const uint32_t r = (group * WAVES + w) * (U * RPI) + u * RPI + rg;
         if (r >= p.rows) return Place{0, 0, -1};
         const uint32_t sh = p.by_n.div(r), s = p.by_h.div(sh);
         return Place{(int)s, (int)(sh - s * p.H), (int)(r - sh * p.n)};
@@ -172,8 +175,13 @@ hipError_t launch_n(CacheRowsParams p, bool store, hipStream_t stream) {
         groups = (uint32_t)p.S * p.H * p.runs;
         p.heads_first = p.sn > p.sh && (int64_t)p.n * p.H >= 1 << 18;
     }
-    return launch_kernel(store ? store_kernel<T, D, U, RUNS, ONCE> : load_kernel<T, D, U, RUNS, ONCE>, dim3(groups),
-                         dim3(64 * WAVES), stream, p);
+    // a launch has fewer than 2^32 threads
+    constexpr uint32_t kMost = 1u << 23;
+    hipError_t e = hipSuccess;
+    for (p.first_group = 0; e == hipSuccess && p.first_group < groups; p.first_group += kMost)
+        e = launch_kernel(store ? store_kernel<T, D, U, RUNS, ONCE> : load_kernel<T, D, U, RUNS, ONCE>,
+                          dim3(std::min(groups - p.first_group, kMost)), dim3(64 * WAVES), stream, p);
+    return e;
 }
 
 // us, D = 128, rows one after the other: 32768 rows by one load instruction a

@@ -27,7 +27,8 @@ struct CacheRowsParams {
     uint32_t rows;                  // S * H * n, at least 1
     Divisor by_n, by_h;
     uint32_t runs;                  // of a head, and
-    bool heads_first;               // their order; set by the launch
+    bool heads_first;               // their order; set by the launch, as is
+    uint32_t first_group;           // the first work-group, of several launches
     void *k, *v;                    // read by a store, written by a load
     int64_t sb, sh, sn;             // element strides shared by k and v
     const int32_t *start, *count;   // [S], or nullptr: 0, n
