@@ -313,7 +313,7 @@ int pi_attn_decode_step_e4m3(int32_t dtype, int32_t S, int32_t H, int32_t D, int
  * Errors: as pi_attn_decode_step, plus EINVAL for plen < 0, pcap < plen, some
  * but not all of the needed byte tables, a null or misaligned k_prefix,
  * v_prefix (plen > 0) or work that is needed; EUNSUPPORTED for S*H of 2^24 and
- * more or plen + cap above 2^31 - 4097.
+ * more (plen > 0: above 2^24 - 8) or plen + cap above 2^31 - 4097.
  */
 int pi_attn_decode_step_prefix(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t plen, int32_t pcap,
                                int32_t cap, int32_t k, int32_t pi, const int32_t *len_in, int32_t *len_out,

@@ -269,9 +269,10 @@ int prepare_decode(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t cap, 
 }
 
 // Sizes that the cached steps' kernels index with 32 bits: positions (with a
-// tile's rows to spare), and a work-group for each (s, h).
+// tile's rows to spare), and a work-group of 256 threads for each (s, h), behind
+// a prefix in a grid of a multiple of 8; a launch has fewer than 2^32 threads.
 bool cached_sizes_ok(int32_t S, int32_t H, int32_t plen, int32_t cap) {
-    return (int64_t)plen + cap <= INT32_MAX - 4096 && (int64_t)S * H < ((int64_t)1 << 24);
+    return (int64_t)plen + cap <= INT32_MAX - 4096 && (int64_t)S * H < ((int64_t)1 << 24) - (plen > 0 ? 7 : 0);
 }
 
 int64_t part_rows(const CachedParams &p) { return (int64_t)(p.chunks + p.own_parts) * p.d.S * p.d.H; }
