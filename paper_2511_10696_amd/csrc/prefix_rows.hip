@@ -535,7 +535,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
     const uint8_t *kbat = p.k_prefix_exp + row_first, *vbat = p.v_prefix_exp + row_first;
     // The bytes of a stage for all: 64 rows a wavefront, the keys' by one half of
     // them, the values' by the other (some of them the same ones).
-    const int byte_row = 64 * (w % (WAVES / 2) % (S::SR / 64)) + lane;
+    const int byte_row = 64 * (w % (WAVES / 2) % (S::SR < 64 ? 1 : S::SR / 64)) + lane;
     if (Q && !S::OWN) kbat = w >= WAVES / 2 ? vbat : kbat;
     int left = plen - stage_row(0);
     const unsigned ring_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)ring;
