@@ -54,7 +54,7 @@ enum {
     PI_ATTN_OK = 0,
     PI_ATTN_EINVAL = -1,       /* null pointer, negative size, bad stride or alignment */
     PI_ATTN_EUNSUPPORTED = -2, /* valid request outside what is built (D, dtype)       */
-    PI_ATTN_EHIP = -3,         /* the HIP runtime refused a launch                      */
+    PI_ATTN_EHIP = -3,         /* a launch was refused: by HIP, or for 2^32 threads or more */
     PI_ATTN_ESCRATCH = -4      /* too large for pi_attn_backward_noalloc's fixed array  */
 };
 

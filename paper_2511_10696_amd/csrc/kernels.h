@@ -12,9 +12,12 @@ namespace pi_attn {
 // Launch through hipLaunchKernel so the launch status is returned directly
 // (no reliance on the per-thread last-error state).  Arguments convert to the
 // kernel's parameter types.
+// A grid of 2^32 threads or more is refused here: the launch would start the
+// remainder only, and report no error.
 template <typename... KArgs>
 inline hipError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t stream,
                                 typename std::common_type<KArgs>::type... args) {
+    if ((uint64_t)grid.x * block.x > UINT32_MAX) return hipErrorInvalidConfiguration;
     void *argv[] = {static_cast<void *>(&args)...};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, block, argv, 0, stream);
 }
