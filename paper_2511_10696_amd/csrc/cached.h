@@ -61,12 +61,6 @@ __host__ __device__ inline int chunk_end(const CachedParams &p, int x) {
     return last + 1 == tiles ? p.plen : p.plen - p.near + (last + 1) * p.tile;
 }
 
-// A logit within [-c, c]; one that is not a number stays so (fminf and fmaxf would make it -c: a key row that is stored as
-// NaN would count with weight exp(-c)).
-__device__ inline float clamped_logit(float x, float c) {
-    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -c), c);
-}
-
 // Decode step of CachedParams: the parts' sizes, then the step.
 void plan_decode_cached(CachedParams &p, bool bf16);
 hipError_t launch_decode_cached(const CachedParams &p, bool bf16, hipStream_t stream);

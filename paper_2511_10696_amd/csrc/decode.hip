@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_kernel(DecodeParams p) {
 #pragma unroll
         for (int e = 0; e < EPL; ++e) part += qf[e] * kf[e];
         part = row_sum<LPR>(part);
-        if constexpr (CLAMP) return fminf(fmaxf(part * p.scale + bias, -p.clamp), p.clamp) * kLog2e;
+        if constexpr (CLAMP) return clamped_logit(part * p.scale + bias, p.clamp) * kLog2e;
         return part * c2 + bias * kLog2e;
     };
 

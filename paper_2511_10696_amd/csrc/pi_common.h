@@ -88,6 +88,13 @@ __device__ inline FusionBias fusion_bias(float g, bool exact) {
     return fb;
 }
 
+// A decode step's logit within [-c, c]; one that is not a number stays so (fminf
+// and fmaxf would make it -c: a key row that holds NaN would count with weight
+// exp(-c)).
+__device__ inline float clamped_logit(float x, float c) {
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -c), c);
+}
+
 // Prior derivatives of one gate logit: d log alpha~/dg and d log(1 - alpha~)/dg.
 struct GateDeriv {
     float local, partner;

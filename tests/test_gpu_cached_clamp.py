@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2511_10696_amd as pa
 from tests.cached_ref import E4M3
 from tests.test_gpu_decode_cached import Problem
 
@@ -54,3 +55,21 @@ def test_new_rows_that_are_not_finite(device, dtype, what):
     want.check(out, p.lse)
     assert bool(torch.isnan(out[1, 1]).all()) and not bool(torch.isnan(out[0]).any())
     assert p.own[0].view(torch.uint8).view(E4M3)[1, 1, 40].float().isnan().sum() == 1
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("k", [3, 60, 300])
+def test_plain_step(device, dtype, D, k):
+    """pi_attn_decode_step, which the others extend: the same."""
+    cap, pi = k + 90, k + 20
+    lens = [0, k, k + 30, k + 60, 2, k + 89]
+    p = Problem(dtype, False, 6, 2, D, 0, cap, k, pi, lens, clamp=4.0)
+    spoil(p.own[0][1], k - 1, False)
+    spoil(p.own[0][2], 30, False)
+    spoil(p.own[0][3], 60 - 20, False)   # a partner
+    p.kn[4, 1, 5] = float("nan")
+    want = p.expected()
+    assert np.array_equal(np.isnan(want.lse).any(1), [False, True, True, True, True, False])
+    lse = torch.empty(6, 2, device="cuda")
+    want.check(pa.pi_attn_decode_step(p.lens, p.q, p.kn, p.vn, *p.own, p.gate, k, pi, logit_clamp=4.0, lse=lse), lse)
