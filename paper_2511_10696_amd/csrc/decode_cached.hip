@@ -397,6 +397,16 @@ hipError_t launch_n(const CachedParams &p, hipStream_t stream) {
 // 29.1, 26.6 and 24.8, of 512 rows 46.8, 47 and 47.4, of 1024 rows 87.0, - and
 // 92.0.  With the parts of a prefix, 2048 (s, h): of 256 rows 44.7, 42.5 and 36.5,
 // of 512 rows 48.0, - and 41.3; bf16 of 256 rows 50.5, - and 48.4.
+// The other types and D, the rule's choice first: from 2048 (s, h) on, 2 wavefronts
+// and 4, e4m3 D = 64 of 65 rows 8.0 and 8.5, of 257 16.1 and 16.9, float32 over
+// e4m3 D = 128 of 129 15.5 and 17.0, parts of a bf16 prefix D = 128 of 129 50 and
+// 51, of a float32 one D = 64 60.6 and 58.0.  From 33 loads on, 8 and 4: e4m3 D =
+// 64, 256 (s, h) of 1025 rows 9.6 and 10.8, bf16 behind chunks D = 128, 128 of 257
+// 22.3 and 23.3, float32 D = 64 18.3 and 19.6; the prefix's rows too, bf16 D = 128,
+// 32 of 520 7.3 and 9.6, float32 D = 64 32 of 420 5.1 and 6.0; 2048 of 513 45.5 and
+// 44.9.  From 5 loads on, up to 1024 (s, h), 4 wavefronts of 4 and 2 of 2: e4m3 D =
+// 128 of 41 rows 32 (s, h) 4.2 and 4.7, 1024 6.5 and 6.2; D = 64 256 of 100 4.4 and
+// 5.4, float32 over e4m3 4.3 and 5.3.
 template <typename T, typename ST, int D, bool CLAMP>
 hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
     const int64_t n = (int64_t)p.d.S * p.d.H;
@@ -413,7 +423,6 @@ hipError_t launch_w(const CachedParams &p, hipStream_t stream) {
                           : launch_n<T, ST, D, CLAMP, DIRECT, 4, 4>(p, stream);
     }
     if (p.chunks) {
-        if (loads <= 8) return launch_n<T, ST, D, CLAMP, WHOLE, 2, 2>(p, stream);
         if (many && loads <= 64) return launch_n<T, ST, D, CLAMP, WHOLE, 2, 4>(p, stream);
         return loads > 32 ? launch_n<T, ST, D, CLAMP, WHOLE, 8, 4>(p, stream)
                           : launch_n<T, ST, D, CLAMP, WHOLE, 4, 4>(p, stream);
