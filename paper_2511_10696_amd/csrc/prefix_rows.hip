@@ -5,9 +5,9 @@
 // Of head h, sequence s at position t = plen + len_in[s] attends the prefix
 // rows max(0, t - k)..plen - 1: an end of the prefix, the same rows for every
 // sequence but for where they begin.  A work-group takes one chunk of the rows
-// of one head and a group of sequences, and leaves for each of them the largest
-// logit m of the chunk (log2 units), l = sum 2^(x - m) and the values weighted
-// alike, o; decode_cached.hip joins the chunks with the sequence's own rows.  A
+// of one head and a group of sequences, and leaves for each of them an m little
+// above the largest logit of the chunk (log2 units), l = sum 2^(x - m) and the
+// values weighted alike, o; decode_cached.hip joins the chunks with the sequence's own rows.  A
 // chunk is every n-th tile of rows, so that whatever the windows leave is shared
 // by all work-groups, and the last tile comes first, which every window that
 // meets the prefix holds: the first loads wait for no length.
@@ -26,13 +26,12 @@
 // As in forward_bf16.hip the scores are computed transposed, S^T = K Q^T, so
 // that a lane holds scores of one query and the probabilities are the B operand
 // of O^T = V^T P^T as they lie, the row order permuted alike in the V^T operand
-// (LDS transpose reads).  The running maximum is raised with every block that
-// has a larger logit.  In bf16 a weight is the sum of two bf16 terms, two
+// (LDS transpose reads).  In bf16 a weight is the sum of two bf16 terms, two
 // products with each value operand, so that outputs are as near the definition
 // as with float32 weights, which a step has that reads its rows with vector
-// instructions.  One term, off by 2^-8, took 75 us where two take 85 (64
-// sequences of 32 heads behind 32768 e4m3 rows, D = 128), 122 and 144 (128
-// behind as many of bf16), 93 and 92 (24 of 16 behind 65536).
+// instructions.  One term, off by 2^-8, took 75 us where two take 81 (64
+// sequences of 32 heads behind 32768 e4m3 rows, D = 128), 122 and 138 (128
+// behind as many of bf16), 92 and 90 (24 of 16 behind 65536).
 //
 // Rows that begin before a sequence's window are masked in the blocks that
 // hold such rows.  A masked weight is 0, but 0 times an infinity or NaN is not:
@@ -373,10 +372,14 @@ struct Mma<float, ST, D, NG> {
     }
 };
 
-// A weight 2^(s c - m) of a score s, m the largest of the rounded s c.  The product is rounded with the difference, which
-// costs nothing and keeps its last bits; but then the largest score's weight is 2^r, r the rounding of m.  WIDE, once some
-// |m| has passed 2^22 (r up to 1/4; at 2^32 it would be 256): rounded first, as m is, so that the largest weight is 1.
+// A weight 2^(s c - m) of a score s, m at least the largest of the rounded s c.  The product is rounded with the
+// difference, which costs nothing and keeps its last bits; but then all weights are off by 2^r, r the rounding of m.  WIDE,
+// once some |m| has passed 2^22 (r up to 1/4; at 2^32 it would be 256): the product is rounded first, as m is.
 constexpr float kWide = 0x1p22f;
+
+// m is set above the largest score so far, so that few later blocks raise it and rescale the state; weights are at most 1
+// either way.  64 sequences of 32 heads behind 32768 e4m3 rows, D = 128, 85 -> 81 us, 128 behind bf16 146 -> 138.
+constexpr float kHeadroom = 4.0f;
 
 template <bool WIDE>
 __device__ inline float weight(float s, float c, float m) {
@@ -694,7 +697,7 @@ __global__ __launch_bounds__(S::NT, (S::TWO || S::WAVES == 8 ? 2 : 1)) void pref
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
                 large |= mx[n] > m[n] && fabsf(mx[n]) > kWide;
-                const float m_new = fmaxf(m[n], mx[n]);
+                const float m_new = mx[n] > m[n] ? mx[n] + kHeadroom : m[n];
                 const float alpha = mx[n] > m[n] ? __builtin_amdgcn_exp2f(m[n] - m_new) : 1.0f;
                 m[n] = m_new;
                 l[n] *= alpha;
