@@ -230,8 +230,8 @@ struct Mma<__bf16, ST, D, NG> {
                 if constexpr (Q) {
                     vf = widen8(vr[cc][b][0].x, vr[cc][b][0].y, 1.0f);
                 } else {
-                    const uint2 lo = vr[cc][b][0], hi = vr[cc][b][1];
-                    vf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                    const uint2 r0 = vr[cc][b][0], r8 = vr[cc][b][1];   // rows from 0 and 8 on
+                    vf = __builtin_bit_cast(bf16x8, make_uint4(r0.x, r0.y, r8.x, r8.y));
                 }
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
