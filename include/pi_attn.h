@@ -229,8 +229,8 @@ int pi_attn_cache_store(int32_t dtype, int32_t S, int32_t H, int32_t D, int32_t 
 /*
  * pi_attn_cache_load -- rows of a quantised cache in the working type: row i <
  * n of k and v is cache row start[s] + i, and zeros where i >= count[s] or that
- * row lies outside [0, cap).  What it returns can go into pi_attn_forward_shard
- * as the rows that a later chunk of the prompt attends.
+ * row lies outside [0, cap).  bf16 rows can go into pi_attn_forward_shard as the
+ * rows that a later chunk of the prompt attends.
  *   Arguments    as pi_attn_cache_store; every row of k and v [S][H][n][D] is
  *                written (through sb, sh, sn, each at least D where its extent
  *                is more than 1), values rounded to dtype (exact but for

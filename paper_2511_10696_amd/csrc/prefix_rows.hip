@@ -29,9 +29,9 @@
 // (LDS transpose reads).  In bf16 a weight is the sum of two bf16 terms, two
 // products with each value operand, so that outputs are as near the definition
 // as with float32 weights, which a step has that reads its rows with vector
-// instructions.  One term, off by 2^-8, took 75 us where two take 81 (64
-// sequences of 32 heads behind 32768 e4m3 rows, D = 128), 122 and 138 (128
-// behind as many of bf16), 92 and 90 (24 of 16 behind 65536).
+// instructions.  One term, off by 2^-8, took 76 us where two take 82 (64
+// sequences of 32 heads behind 32768 e4m3 rows, D = 128), 121 and 137 (128
+// behind as many of bf16), 93 and 93 (24 of 16 behind 65536).
 //
 // Rows that begin before a sequence's window are masked in the blocks that
 // hold such rows.  A masked weight is 0, but 0 times an infinity or NaN is not:
@@ -42,12 +42,12 @@
 // registers.)
 //
 // What bounds it, whole steps: HBM in bf16 (24 sequences of 16 heads behind 65536
-// rows, D = 128: 537 MB in 91 us, 5.9 TB/s; 64 of 32 behind 32768: 96 us) and in
-// e4m3 up to 32 sequences (32 of 32 heads behind 32768 rows: 271 MB in 58 us);
-// with 64 of e4m3 the softmax and the conversions, which overlap the loads only in
-// part (79 us; the loads alone 60, the arithmetic alone 61); from 128 the matrix
-// and the softmax instructions (bf16 127 us, e4m3 121); in float32 the products
-// (64 of 32 behind 8192: 97 us, 88 TFLOP/s).  Short of that the two launches, a
+// rows, D = 128: 537 MB in 93 us, 5.8 TB/s; 64 of 32 behind 32768: 98 us) and in
+// e4m3 up to 32 sequences (32 of 32 heads behind 32768 rows: 271 MB in 59 us); with
+// 64 of e4m3 softmax, products and conversions, which overlap the loads only in
+// part (82 us, with the rows in the caches 75); from 128 the matrix and the softmax
+// instructions (bf16 137 us, e4m3 132); in float32 the products (64 of 32 behind
+// 8192: 96 us, 89 TFLOP/s; over e4m3 104).  Short of that the two launches, a
 // round trip each, and the parts, 17 MB written and read again at 64 of 32 heads.
 #include "bf16_rows.h"
 #include "cached.h"
