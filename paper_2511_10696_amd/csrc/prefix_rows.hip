@@ -7,10 +7,11 @@
 // sequence but for where they begin.  A work-group takes one chunk of the rows
 // of one head and a group of sequences, and leaves for each of them an m little
 // above the largest logit of the chunk (log2 units), l = sum 2^(x - m) and the
-// values weighted alike, o; decode_cached.hip joins the chunks with the sequence's own rows.  A
-// chunk is every n-th tile of rows, so that whatever the windows leave is shared
-// by all work-groups, and the last tile comes first, which every window that
-// meets the prefix holds: the first loads wait for no length.
+// values weighted alike, o; decode_cached.hip joins the chunks with the
+// sequence's own rows.  A chunk is every n-th tile of rows, so that whatever the
+// windows leave is shared by all work-groups, and the last tile comes first,
+// which every window that meets the prefix holds: the first loads wait for no
+// length.
 //
 // Rows go from global memory straight into LDS as they are stored, through a
 // ring of stages: while a stage is worked on, the next ones are on their way,
