@@ -497,6 +497,148 @@ int pi_attn_backward_shard_kv(int32_t dtype, int32_t B, int32_t H, int32_t D, in
  */
 int pi_attn_gate_grad_per_head(int32_t B, int32_t H, int32_t N, const float *dgate, float *out, void *stream);
 
+/*
+ * Rotary positions.  A row of D elements is D/2 pairs, pair i its elements i and
+ * i + D/2.  The first n0 pairs belong to axis 0, the next n1 to axis 1, the next
+ * n2 to axis 2 (time, height and width; one axis: n1 = n2 = 0), and pair i of
+ * axis a is turned by the angle pos_a * freq[i]:
+ *   y_i       = x_i cos - x_(i + D/2) sin
+ *   y_(i+D/2) = x_i sin + x_(i + D/2) cos.
+ * Pairs from n0 + n1 + n2 <= D/2 on stay as they are, bit by bit.  Angles are formed
+ * in 64 bits from the float32 frequencies, the rest is fp32 with one rounding at
+ * the end.
+ *
+ * pi_attn_rotate -- q and k turned by their positions, or back.
+ *   dtype, out_dtype   of q, k and of q_out, k_out.
+ *   B, H, Hk, N, D     sequences, heads of q and of k (either may be 0, its
+ *                tensors are not looked at then), positions, head dimension.
+ *   back         non-zero: by the angles' negatives.  A rotation's transpose is its
+ *                inverse, so this is the backward: dL/dq from dL/dq_out.
+ *   q, k         device [B][H][N][D], [B][Hk][N][D] through element strides (qsb,
+ *                qsh, qsn), (ksb, ksh, ksn), the D elements contiguous.
+ *   pos          device int32 positions, pos[a*psa + b*psb + n*psn] on axis a (any
+ *                value, negative ones too), or NULL: n, on every axis.
+ *   freq         device float32 [n0 + n1 + n2], radians a position; NULL: nothing
+ *                is turned.
+ *   q_out, k_out through (oqsb, ...), (oksb, ...), each at least D where its extent
+ *                is more than 1.  Either may be its input itself (same pointer,
+ *                type and strides); otherwise nothing may overlap.
+ * Errors: EINVAL (null or misaligned pointer of a non-empty tensor, negative size or
+ * stride, rows of an output that meet, an output at its input with other strides or
+ * type, n0 + n1 + n2 > D/2, B*N*(H + Hk) of 2^31 and more), EUNSUPPORTED (D not
+ * 64/128, unknown dtype), EHIP (launch refused).
+ */
+int pi_attn_rotate(int32_t dtype, int32_t out_dtype, int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t D, int32_t back,
+                   const void *q, int64_t qsb, int64_t qsh, int64_t qsn, const void *k, int64_t ksb, int64_t ksh,
+                   int64_t ksn, const int32_t *pos, int64_t psa, int64_t psb, int64_t psn, const float *freq, int32_t n0,
+                   int32_t n1, int32_t n2, void *q_out, int64_t oqsb, int64_t oqsh, int64_t oqsn, void *k_out,
+                   int64_t oksb, int64_t oksh, int64_t oksn, void *stream);
+
+/*
+ * Paged caches.  Rows lie in pages of `page` positions, [n_pages][Hk][page][D] for the
+ * keys and for the values: position j of sequence s is row j mod page of page
+ * table[s][j / page].  A table entry outside [0, n_pages) names no page: its
+ * positions have no rows.  Pages hold rows in dtype, or (k_exp not NULL) e4m3 codes
+ * with bytes [n_pages][Hk][page], as quantised caches do.  Sequences may share pages
+ * that nothing writes to.
+ *
+ * pi_attn_paged_store -- rows of a prompt, or of a chunk of one, into a paged cache:
+ * row i < min(count[s], n) of k and v becomes position start[s] + i, the keys turned
+ * by their positions on the way (see pi_attn_rotate; the result is rounded once, to
+ * what the page holds).
+ *   dtype        PI_ATTN_F32 or PI_ATTN_BF16: element type of k and v.
+ *   S, Hk, D, n  sequences, key heads, head dimension, rows given for each.
+ *   n_pages, page, max_pages   pages in all, positions of one, entries of a
+ *                sequence in the table (each >= 1).
+ *   k, v         device [S][Hk][n][D] through element strides (sb, sh, sn) shared by
+ *                both, the D elements contiguous.
+ *   start, count device int32 [S], or NULL for 0, n (negative count: none).
+ *   table        device int32 [S][max_pages].
+ *   k_pages, v_pages, k_exp, v_exp   the cache.
+ *   freq, n0, n1, n2   as in pi_attn_rotate; freq NULL: the keys are stored as
+ *                they are.
+ *   pos          device int32 pos[a*psa + s*psb + i*psn] of row i, or NULL: start[s]
+ *                + i on every axis.
+ * A row without a place (past the table's reach, before position 0, or in no page)
+ * is dropped; every other row of the cache is left as it was.  Two rows of a call must
+ * not have the same place.
+ * Errors: EINVAL (null pointer with rows to store, negative size or stride,
+ * misalignment, one of k_exp and v_exp without the other, n0 + n1 + n2 > D/2, S*Hk*n
+ * of 2^31 and more), EUNSUPPORTED (D not 64/128, unknown dtype, page * max_pages above
+ * 2^31 - 4097), EHIP (launch refused).
+ */
+int pi_attn_paged_store(int32_t dtype, int32_t S, int32_t Hk, int32_t D, int32_t n, int32_t n_pages, int32_t page,
+                        int32_t max_pages, const void *k, const void *v, int64_t sb, int64_t sh, int64_t sn,
+                        const int32_t *start, const int32_t *count, const int32_t *table, void *k_pages, void *v_pages,
+                        uint8_t *k_exp, uint8_t *v_exp, const float *freq, int32_t n0, int32_t n1, int32_t n2,
+                        const int32_t *pos, int64_t psa, int64_t psb, int64_t psn, void *stream);
+
+/*
+ * pi_attn_paged_load -- rows of a paged cache in sequence and in dtype: row i < n of
+ * k and v is position start[s] + i, and zeros where i >= count[s] or that position has
+ * no row.  bf16 rows can go into pi_attn_forward_shard as the rows that a later chunk
+ * of the prompt attends.
+ *   Arguments    as pi_attn_paged_store; every row of k and v [S][Hk][n][D] is written
+ *                (through sb, sh, sn, each at least D where its extent is more than
+ *                1).  Pages in dtype are copied bit by bit.
+ * Errors: as pi_attn_paged_store, and EINVAL for rows of k and v that meet.
+ */
+int pi_attn_paged_load(int32_t dtype, int32_t S, int32_t Hk, int32_t D, int32_t n, int32_t n_pages, int32_t page,
+                       int32_t max_pages, const void *k_pages, const void *v_pages, const uint8_t *k_exp,
+                       const uint8_t *v_exp, const int32_t *start, const int32_t *count, const int32_t *table, void *k,
+                       void *v, int64_t sb, int64_t sh, int64_t sn, void *stream);
+
+/*
+ * pi_attn_paged_workspace -- float32 elements of workspace that
+ * pi_attn_decode_step_paged needs for these sizes; 0 if none, -1 for sizes that it
+ * refuses.  The contents never matter between calls; calls that may run at the same
+ * time need one each.
+ */
+int64_t pi_attn_paged_workspace(int32_t dtype, int32_t S, int32_t H, int32_t Hk, int32_t D, int32_t page,
+                                int32_t max_pages, int32_t k);
+
+/*
+ * pi_attn_decode_step_paged -- pi_attn_decode_step over a paged cache, with shared key
+ * heads and rotary positions: for each sequence s, with t = len_in[s], q_new and k_new
+ * are turned by the sequence's position, the new key/value is stored as position t
+ * (rounded, or quantised, to what the page holds) and the new queries attend over W_t
+ * with every row as it is stored, the new one too.  Query head h belongs to key head
+ * h / (H / Hk).  Positions of W_t that have no row (their page was given back) are
+ * not in it.
+ *   dtype        of q_new, k_new, v_new and out.
+ *   S, H, Hk, D  sequences, query heads, key heads (H a multiple of Hk), head
+ *                dimension.
+ *   n_pages, page, max_pages, table, k_pages, v_pages, k_exp, v_exp   the cache;
+ *                position t of every key head is overwritten, nothing else is written.
+ *                The page of position t must belong to sequence s alone.
+ *   k, pi        window radius and partner period.
+ *   len_in       device int32 [S]: rows so far.
+ *   len_out      optional device int32 [S]: receives len_in[s] + 1; must not overlap
+ *                len_in.
+ *   q_new        device [S][H][D], k_new, v_new [S][Hk][D], contiguous.
+ *   freq, n0, n1, n2   as in pi_attn_rotate; freq NULL: nothing is turned.
+ *   pos          device int32 pos[a*psa + s*pss], or NULL: t on every axis.
+ *   gate         device float32 gate logits gate[s*gss + h*gsh].
+ *   out          device [S][H][D] contiguous; lse optional float32 [S][H].
+ *   work         device float32, 16-byte aligned, of pi_attn_paged_workspace(dtype,
+ *                S, H, Hk, D, page, max_pages, k) elements; may be NULL when that is 0.
+ * A length outside [0, page * max_pages), or whose position has no page: NaN for that
+ * sequence's outputs, the cache untouched, len_out[s] = len_in[s].  Long windows of a
+ * few (s, key head) are split over work-groups, in two launches; the sums are taken in
+ * a fixed order either way, and which kernels run depends on the sizes alone.
+ * Errors: EINVAL (null pointer, negative size, H not a multiple of Hk, misalignment, one
+ * of k_exp and v_exp without the other, n0 + n1 + n2 > D/2, a null or misaligned work
+ * that is needed), EUNSUPPORTED (D not 64/128, unknown dtype, page * max_pages above
+ * 2^31 - 4097, S*H of 2^24 and more), EHIP (launch refused).
+ */
+int pi_attn_decode_step_paged(int32_t dtype, int32_t S, int32_t H, int32_t Hk, int32_t D, int32_t n_pages, int32_t page,
+                              int32_t max_pages, int32_t k, int32_t pi, const int32_t *len_in, int32_t *len_out,
+                              const void *q_new, const void *k_new, const void *v_new, const int32_t *table,
+                              void *k_pages, void *v_pages, uint8_t *k_exp, uint8_t *v_exp, const float *freq, int32_t n0,
+                              int32_t n1, int32_t n2, const int32_t *pos, int64_t psa, int64_t pss, const float *gate,
+                              int64_t gss, int64_t gsh, float scale, float logit_clamp, void *out, float *lse,
+                              float *work, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,11 @@ bidirectional mode, window |j - t| <= k and partners t -/+ pi):
     pi_attn_cache_load(k_cache, v_cache, k_exp, v_exp, n, start=None, count=None)   -> k, v [S,H,n,D]
     pi_attn_decode_step_e4m3(len_in, q_new, k_new, v_new, k_cache, v_cache, k_exp, v_exp, gate, k, pi)
     pi_attn_decode_step_prefix(len_in, q_new, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, gate, k, pi)
+    pi_attn_rotate(q, k, pos, freq, sections=None)            -> q, k turned by their positions
+    pi_attn_rotate_backward(dq, dk, pos, freq, sections=None) -> their gradients
+    pi_attn_paged_store(k, v, k_pages, v_pages, table, start=None, count=None, freq=None)
+    pi_attn_paged_load(k_pages, v_pages, table, n, start=None, count=None)          -> k, v [S,Hk,n,D]
+    pi_attn_decode_step_paged(len_in, q_new, k_new, v_new, k_pages, v_pages, table, gate, k, pi, freq=None)
 Quantised caches are torch.float8_e4m3fn codes [S,H,cap,D] with a torch.uint8
 scale byte for each row [S,H,cap].
 
@@ -41,6 +46,8 @@ __all__ = ["pi_attn_index_set", "pi_attn_forward", "pi_attn_forward_gated", "pi_
            "pi_attn_decode_step", "pi_attn_ws_width",
            "pi_attn_cache_store", "pi_attn_cache_load", "pi_attn_decode_step_e4m3", "pi_attn_decode_step_prefix",
            "pi_attn_decode_workspace",
+           "pi_attn_rotate", "pi_attn_rotate_backward", "pi_attn_paged_store", "pi_attn_paged_load",
+           "pi_attn_paged_workspace", "pi_attn_decode_step_paged",
            "pi_attn_forward_shard", "pi_attn_backward_shard_q", "pi_attn_backward_shard_kv",
            "pi_attn_strerror", "library", "LIB_PATH", "EXPORTED_SYMBOLS", "PiAttnError"]
 
@@ -51,7 +58,8 @@ EXPORTED_SYMBOLS = ("pi_attn_strerror", "pi_attn_ws_width", "pi_attn_default_sca
                     "pi_attn_gate_grad_per_head", "pi_attn_forward_shard", "pi_attn_backward_shard_q",
                     "pi_attn_backward_shard_kv", "pi_attn_backward_noalloc", "pi_attn_cache_store",
                     "pi_attn_cache_load", "pi_attn_decode_workspace", "pi_attn_decode_step_e4m3",
-                    "pi_attn_decode_step_prefix")
+                    "pi_attn_decode_step_prefix", "pi_attn_rotate", "pi_attn_paged_store", "pi_attn_paged_load",
+                    "pi_attn_paged_workspace", "pi_attn_decode_step_paged")
 
 PI_ATTN_F32, PI_ATTN_BF16 = 0, 1
 
@@ -102,6 +110,19 @@ def library() -> ctypes.CDLL:
             lib.pi_attn_decode_step_e4m3.restype = ctypes.c_int
             lib.pi_attn_decode_step_prefix.argtypes = ([i32] * 9 + [vp] * 14 + [i64, i64, f32, f32, vp, vp, vp, vp])
             lib.pi_attn_decode_step_prefix.restype = ctypes.c_int
+            lib.pi_attn_rotate.argtypes = ([i32] * 8 + [vp, i64, i64, i64] * 3 + [vp, i32, i32, i32]
+                                           + [vp, i64, i64, i64] * 2 + [vp])
+            lib.pi_attn_rotate.restype = ctypes.c_int
+            lib.pi_attn_paged_store.argtypes = ([i32] * 8 + [vp, vp, i64, i64, i64] + [vp] * 7
+                                                + [vp, i32, i32, i32, vp, i64, i64, i64, vp])
+            lib.pi_attn_paged_store.restype = ctypes.c_int
+            lib.pi_attn_paged_load.argtypes = [i32] * 8 + [vp] * 9 + [i64, i64, i64, vp]
+            lib.pi_attn_paged_load.restype = ctypes.c_int
+            lib.pi_attn_paged_workspace.argtypes = [i32] * 8
+            lib.pi_attn_paged_workspace.restype = i64
+            lib.pi_attn_decode_step_paged.argtypes = ([i32] * 10 + [vp] * 10 + [vp, i32, i32, i32, vp, i64, i64]
+                                                      + [vp, i64, i64, f32, f32, vp, vp, vp, vp])
+            lib.pi_attn_decode_step_paged.restype = ctypes.c_int
             lib.pi_attn_backward.argtypes = ([i32] * 8 + [vp, vp, vp, i64, i64, i64, vp, i64, i64, i64,
                                                          f32, f32, vp, vp, vp, i64, i64, i64,
                                                          vp, vp, vp, vp, vp, vp])
@@ -138,6 +159,7 @@ class _PythonOnly:
 
     forward_gated = backward = decode_step = forward
     cache_store = cache_load = decode_step_e4m3 = decode_step_prefix = forward
+    rotate = paged_store = paged_load = decode_step_paged = forward
 
 
 def _load_native():
@@ -891,3 +913,270 @@ def _prefix_checked(k_prefix, v_prefix, dtype, H, D):
     if rest or pcap < plen:
         raise ValueError("the heads of k_prefix must lie whole rows apart, at least plen")
     return plen, _int32("the rows between the heads of k_prefix", pcap)
+
+
+def _rotary(torch, freq, sections, pos, shape, D):
+    """The rotation's arguments: (freq, pairs of each of three axes, pos, its strides), for positions of
+    ``shape`` ((B, N), or (S,) in a decode step); pos has an axis before these, or none for one axis."""
+    none = (0,) * (1 + len(shape))
+    if freq is None:
+        if pos is not None or sections is not None:
+            raise ValueError("pos and sections go with freq")
+        return None, (0, 0, 0), None, none
+    if freq.dtype != torch.float32 or freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError("freq must be a contiguous float32 tensor, a frequency for each pair")
+    sections = (freq.shape[0],) if sections is None else tuple(int(x) for x in sections)
+    if not 1 <= len(sections) <= 3 or min(sections) < 0 or sum(sections) != freq.shape[0]:
+        raise ValueError("sections must be the pairs of one to three axes, which freq has one frequency for each of")
+    if sum(sections) > D // 2:
+        raise ValueError(f"a row of {D} elements has {D // 2} pairs")
+    pairs = sections + (0,) * (3 - len(sections))
+    if pos is None:
+        return freq, pairs, None, none
+    if pos.dtype != torch.int32:
+        raise TypeError("pos must be int32")
+    full = (len(sections),) + tuple(shape)
+    if len(sections) == 1 and pos.dim() <= len(shape):
+        at = pos.dim()
+        if at == 0 or tuple(pos.shape) != tuple(shape[len(shape) - at:]):
+            raise ValueError(f"pos must be {list(full)} or {list(shape)}, got {list(pos.shape)}")
+        strides = (0,) * (len(full) - at) + tuple(pos.stride())
+    elif tuple(pos.shape) != full:
+        raise ValueError(f"pos must be {list(full)}, got {list(pos.shape)}")
+    else:
+        strides = tuple(pos.stride())
+    return freq, pairs, pos, strides
+
+
+def _rotate(q, k, pos, freq, sections, dtype, q_out, k_out, stream, back, where):
+    r = (_native or _load_native()).rotate(q, k, pos, freq, sections, dtype, q_out, k_out, stream, back)
+    if r is not None:
+        return r
+    torch = _torch()
+    _require_cuda(q, k, pos, freq, q_out, k_out)
+    _same_device(q, k, pos, freq, q_out, k_out)
+    B, _, N, D = _heads_checked(q, "q")
+    if k is not None:
+        if k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (B, N, D) or k.stride(3) != 1 or k.dtype != q.dtype:
+            raise ValueError(f"k must be a [{B}, heads, {N}, {D}] tensor of q's dtype with a contiguous last dimension")
+    elif k_out is not None:
+        raise ValueError("k_out goes with k")
+    freq, pairs, pos, ps = _rotary(torch, freq, sections, pos, (B, N), D)
+    given = q_out if q_out is not None else k_out
+    dtype = dtype if dtype is not None else given.dtype if given is not None else q.dtype
+    code = _dtype_code(q.dtype), _dtype_code(dtype)
+    outs = []
+    for name, x, out in (("q_out", q, q_out), ("k_out", k, k_out)):
+        if x is not None and out is None:
+            with _on(stream):
+                out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        if out is not None and (out.shape != x.shape or out.dtype != dtype or out.stride(3) != 1):
+            raise ValueError(f"{name} must be a {dtype} {list(x.shape)} tensor with a contiguous last dimension")
+        outs.append(out)
+
+    H, Hk = q.shape[1], 0 if k is None else k.shape[1]
+    with torch.cuda.device(q.device):
+        st = library().pi_attn_rotate(
+            *code, *(_int32(*x) for x in (("B", B), ("H", H), ("Hk", Hk), ("N", N))), D, int(back), _ptr(q), *_row_strides(q), _ptr(k),
+            *_row_strides(k), _ptr(pos), *ps, _ptr(freq), *pairs, _ptr(outs[0]), *_row_strides(outs[0]), _ptr(outs[1]),
+            *_row_strides(outs[1]), _stream_handle(stream, q.device))
+    _check(st, where)
+    return tuple(outs)
+
+
+def _row_strides(x):
+    """Element strides of the rows of x [.., .., .., D] (or None): 0 where there is one alone."""
+    return (0, 0, 0) if x is None else tuple(st if n > 1 else 0 for n, st in zip(x.shape[:3], x.stride()))
+
+
+def _heads_checked(x, name):
+    if x.dim() != 4 or x.stride(3) != 1:
+        raise ValueError(f"{name} must be a [B, heads, N, D] tensor with a contiguous last dimension")
+    return x.shape
+
+
+def pi_attn_rotate(q, k, pos, freq, sections=None, dtype=None, q_out=None, k_out=None, stream=None):
+    """Rotary positions: pair i of a row (its elements i and i + D/2) turned by
+    the angle pos * freq[i], for the queries and keys of pi_attn_forward.
+
+    q [B, H, N, D], k [B, Hk, N, D] or None: float32 or bfloat16, any strides with
+    a contiguous last dimension.  freq: float32 [P], P <= D/2, radians a position;
+    pairs from P on stay as they are.  sections: the pairs of each axis, one to
+    three whole numbers that sum to P (time, height and width: the first pairs
+    belong to axis 0, the next to axis 1, ...); None: one axis.  pos: int32
+    [axes, B, N], for one axis [B, N] or [N] too, any strides; None: 0..N-1.
+    Angles are formed in 64 bits.  Returns (q, k) turned, contiguous and in
+    ``dtype`` (the inputs'), or in q_out, k_out; either may be its input itself.
+    """
+    return _rotate(q, k, pos, freq, sections, dtype, q_out, k_out, stream, False, "pi_attn_rotate")
+
+
+def pi_attn_rotate_backward(dq, dk, pos, freq, sections=None, dtype=None, dq_out=None, dk_out=None, stream=None):
+    """Gradients of pi_attn_rotate's inputs from those of its results, for
+    instance the dq and dk of pi_attn_backward: turned back by the same angles.
+    Arguments as pi_attn_rotate; ``dtype``: the gradients' type, that of dq and dk
+    if none is given."""
+    return _rotate(dq, dk, pos, freq, sections, dtype, dq_out, dk_out, stream, True, "pi_attn_rotate_backward")
+
+
+def _pages_checked(torch, k_pages, v_pages, table, k_exp, v_exp, dtype):
+    """The sizes of a paged cache: n_pages, Hk, page, D, S, max_pages."""
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must share one [pages, Hk, page, D] shape")
+    quantised = k_pages.dtype == torch.float8_e4m3fn
+    if v_pages.dtype != k_pages.dtype or not quantised and k_pages.dtype != dtype:
+        raise TypeError("pages must be in the rows' dtype, or float8_e4m3fn")
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        raise ValueError("pages must be contiguous")
+    if (k_exp is not None) != quantised or (v_exp is not None) != quantised:
+        raise ValueError("k_exp and v_exp belong to float8_e4m3fn pages, both")
+    for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+        if t is not None and (t.dtype != torch.uint8 or t.shape != k_pages.shape[:3] or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous uint8 [pages, Hk, page] tensor")
+    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 [S, pages of a sequence] tensor")
+    n_pages, Hk, page, D = k_pages.shape
+    sizes = (_int32(*x) for x in (("pages", n_pages), ("Hk", Hk), ("page", page)))
+    return (*sizes, D, _int32("S", table.shape[0]), _int32("pages of a sequence", table.shape[1]))
+
+
+def pi_attn_paged_store(k, v, k_pages, v_pages, table, start=None, count=None, k_exp=None, v_exp=None, freq=None,
+                        pos=None, sections=None, stream=None):
+    """Stores rows in a paged cache: row i < min(count[s], n) of k and v
+    [S, Hk, n, D] (float32 or bfloat16, identical strides, last dimension
+    contiguous) becomes position start[s] + i of sequence s, the keys turned by
+    their positions on the way if freq is given.
+
+    k_pages, v_pages: [pages, Hk, page, D] in the rows' dtype, or float8_e4m3fn with
+    the scale bytes k_exp, v_exp uint8 [pages, Hk, page] (see pi_attn_cache_store).
+    table: int32 [S, pages of a sequence]: position j lies in page table[s, j //
+    page], row j % page; an entry that names no page has no rows.  start, count:
+    int32 [S] on the GPU (0 and n).  freq, sections: as in pi_attn_rotate; pos: int32
+    [axes, S, n], for one axis [S, n] or [n] too, None: the positions themselves.
+    Rows without a place are dropped, all others of the cache are left as they were.
+    """
+    r = (_native or _load_native()).paged_store(k, v, k_pages, v_pages, table, start, count, k_exp, v_exp, freq, pos,
+                                                sections, stream)
+    if r is not None:
+        return
+    torch = _torch()
+    ts = (k, v, k_pages, v_pages, table, start, count, k_exp, v_exp, freq, pos)
+    _require_cuda(*ts)
+    _same_device(*ts)
+    n_pages, Hk, page, D, S, max_pages = _pages_checked(torch, k_pages, v_pages, table, k_exp, v_exp, k.dtype)
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+        raise ValueError("k and v must share one [S, Hk, n, D] shape, dtype and strides")
+    if (k.shape[0], k.shape[1], k.shape[3]) != (S, Hk, D) or k.stride(3) != 1:
+        raise ValueError(f"k and v must be [{S}, {Hk}, n, {D}] with a contiguous last dimension")
+    _per_sequence(torch, start, S, "start")
+    _per_sequence(torch, count, S, "count")
+    n = _int32("n", k.shape[2])
+    freq, pairs, pos, ps = _rotary(torch, freq, sections, pos, (S, n), D)
+    with torch.cuda.device(k.device):
+        st = library().pi_attn_paged_store(
+            _dtype_code(k.dtype), S, Hk, D, n, n_pages, page, max_pages, _ptr(k), _ptr(v), *_row_strides(k), _ptr(start),
+            _ptr(count), _ptr(table), _ptr(k_pages), _ptr(v_pages), _ptr(k_exp), _ptr(v_exp), _ptr(freq), *pairs,
+            _ptr(pos), *ps, _stream_handle(stream, k.device))
+    _check(st, "pi_attn_paged_store")
+
+
+def pi_attn_paged_load(k_pages, v_pages, table, n: int, start=None, count=None, k_exp=None, v_exp=None, dtype=None,
+                       k=None, v=None, stream=None):
+    """Rows of a paged cache (see pi_attn_paged_store) in sequence: row i < n of
+    the returned k and v [S, Hk, n, D] is position start[s] + i, and zeros where i >=
+    count[s] or that position has no row.  dtype: that of the pages, or for
+    float8_e4m3fn pages that of the given outputs, bfloat16 without any; k, v: outputs to write
+    to (identical strides, last dimension contiguous)."""
+    r = (_native or _load_native()).paged_load(k_pages, v_pages, table, n, start, count, k_exp, v_exp, dtype, k, v,
+                                               stream)
+    if r is not None:
+        return r
+    torch = _torch()
+    ts = (k_pages, v_pages, table, start, count, k_exp, v_exp, k, v)
+    _require_cuda(*ts)
+    _same_device(*ts)
+    if dtype is None:
+        given = v if k is None else k
+        dtype = (given.dtype if given is not None else torch.bfloat16 if k_pages.dtype == torch.float8_e4m3fn
+                 else k_pages.dtype)
+    n_pages, Hk, page, D, S, max_pages = _pages_checked(torch, k_pages, v_pages, table, k_exp, v_exp, dtype)
+    n = _int32("n", n)
+    if n < 0:
+        raise ValueError("n must not be negative")
+    with _on(stream):
+        if k is None:
+            k = torch.empty((S, Hk, n, D), dtype=dtype, device=k_pages.device) if v is None else torch.empty_like(v)
+        if v is None:
+            v = torch.empty_like(k)
+    for t in (k, v):
+        if tuple(t.shape) != (S, Hk, n, D) or t.dtype != dtype or t.stride() != k.stride() or t.stride(3) != 1:
+            raise ValueError(f"k and v must be {dtype} [{S}, {Hk}, {n}, {D}] tensors that share strides, with a "
+                             "contiguous last dimension")
+    _per_sequence(torch, start, S, "start")
+    _per_sequence(torch, count, S, "count")
+    with torch.cuda.device(k_pages.device):
+        st = library().pi_attn_paged_load(
+            _dtype_code(dtype), S, Hk, D, n, n_pages, page, max_pages, _ptr(k_pages), _ptr(v_pages), _ptr(k_exp),
+            _ptr(v_exp), _ptr(start), _ptr(count), _ptr(table), _ptr(k), _ptr(v), *_row_strides(k),
+            _stream_handle(stream, k.device))
+    _check(st, "pi_attn_paged_load")
+    return k, v
+
+
+def pi_attn_paged_workspace(dtype, S: int, H: int, Hk: int, D: int, page: int, max_pages: int, k: int) -> int:
+    """float32 elements of workspace that a step of pi_attn_decode_step_paged needs."""
+    sizes = [_int32(*x) for x in (("S", S), ("H", H), ("Hk", Hk), ("D", D), ("page", page), ("max_pages", max_pages),
+                                  ("k", k))]
+    n = int(library().pi_attn_paged_workspace(_dtype_code(dtype), *sizes))
+    if n < 0:
+        raise PiAttnError(-1, "pi_attn_paged_workspace")
+    return n
+
+
+def pi_attn_decode_step_paged(len_in, q_new, k_new, v_new, k_pages, v_pages, table, gate, k: int, pi: int, k_exp=None,
+                              v_exp=None, freq=None, pos=None, sections=None, scale: float | None = None,
+                              logit_clamp: float = 0.0, len_out=None, out=None, lse=None, work=None, stream=None):
+    """One decode step over a paged cache (see pi_attn_paged_store): stores k_new/v_new
+    [S, Hk, D] as position len_in[s] of each sequence and attends q_new [S, H, D] over
+    its working set, H / Hk query heads to a key head, both turned by their
+    positions first if freq is given (sections: as in pi_attn_rotate; pos: int32
+    [axes, S], for one axis [S] too, None: len_in).  Rows of pages that are not there
+    (given back) are left out.  gate: float32 [H] or [S, H].  work: a float32 workspace of
+    pi_attn_paged_workspace(q_new.dtype, S, H, Hk, D, page, pages of a sequence, k)
+    elements, or None to have it allocated.  Returns out [S, H, D]."""
+    r = (_native or _load_native()).decode_step_paged(
+        len_in, q_new, k_new, v_new, k_pages, v_pages, table, gate, k, pi, k_exp, v_exp, freq, pos, sections, scale,
+        logit_clamp, len_out, out, lse, work, stream)
+    if r is not None:
+        return r
+    torch = _torch()
+    ts = (len_in, q_new, k_new, v_new, k_pages, v_pages, table, gate, k_exp, v_exp, freq, pos, len_out, out, lse, work)
+    _require_cuda(*ts)
+    _same_device(*ts)
+    n_pages, Hk, page, D, S, max_pages = _pages_checked(torch, k_pages, v_pages, table, k_exp, v_exp, q_new.dtype)
+    if q_new.dim() != 3 or q_new.shape[0] != S or q_new.shape[2] != D or not q_new.is_contiguous():
+        raise ValueError(f"q_new must be a contiguous [{S}, H, {D}] tensor")
+    H = _int32("H", q_new.shape[1])
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if tuple(t.shape) != (S, Hk, D) or not t.is_contiguous() or t.dtype != q_new.dtype:
+            raise ValueError(f"{name} must be a contiguous [{S}, {Hk}, {D}] tensor of q_new's dtype")
+    if Hk == 0 or H % Hk:
+        raise ValueError("the query heads must be a multiple of the key heads")
+    out, (gss, gsh) = _step_checked(torch, len_in, q_new, q_new, q_new, S, H, D, gate, len_out, out, lse, stream)
+    freq, pairs, pos, ps = _rotary(torch, freq, sections, pos, (S,), D)
+    k, pi = _int32("k", k), _int32("pi", pi)
+    code = _dtype_code(q_new.dtype)
+    need = int(library().pi_attn_paged_workspace(code, S, H, Hk, D, page, max_pages, k))
+    if work is None and need > 0:
+        with torch.cuda.device(q_new.device), _on(stream):
+            work = torch.empty(need, dtype=torch.float32, device=q_new.device)
+    elif work is not None and (work.dtype != torch.float32 or not work.is_contiguous() or work.numel() < need):
+        raise ValueError(f"work must be a contiguous float32 tensor of at least {need} elements")
+    with torch.cuda.device(q_new.device):
+        st = library().pi_attn_decode_step_paged(
+            code, S, H, Hk, D, n_pages, page, max_pages, k, pi, _ptr(len_in), _ptr(len_out), _ptr(q_new), _ptr(k_new),
+            _ptr(v_new), _ptr(table), _ptr(k_pages), _ptr(v_pages), _ptr(k_exp), _ptr(v_exp), _ptr(freq), *pairs, _ptr(pos),
+            *ps, _ptr(gate), gss, gsh, _scale(scale, D), float(logit_clamp), _ptr(out), _ptr(lse), _ptr(work),
+            _stream_handle(stream, q_new.device))
+    _check(st, "pi_attn_decode_step_paged")
+    return out

@@ -7,6 +7,7 @@
 
 #include "../../include/pi_attn.h"
 #include "cached.h"
+#include "checks.h"
 #include "kernels.h"
 #include "pi_common.h"
 #include "smallk.h"
@@ -14,17 +15,6 @@
 using namespace pi_attn;
 
 namespace {
-
-constexpr int64_t kMaxRows = (int64_t)1 << 31;   // B*H*N (and S*H) limit
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-int elem_size(int32_t dtype) { return dtype == PI_ATTN_F32 ? 4 : dtype == PI_ATTN_BF16 ? 2 : 0; }
-
-bool stride16(int64_t stride_elems, int es) { return stride_elems >= 0 && ((stride_elems * es) & 15) == 0; }
-
-int from_hip(hipError_t e) { return e == hipSuccess ? PI_ATTN_OK : PI_ATTN_EHIP; }
 
 // The bf16 kernels address the key/value rows one tile of 128 queries (or
 // keys) can reach -- at most k + 256 of them, 2k + 256 bidirectional --

@@ -26,6 +26,7 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <array>
 #include <cmath>
 #include <string>
@@ -560,6 +561,274 @@ PyObject *decode_step_prefix(PyObject *self, PyObject *const *args, Py_ssize_t n
     END_HANDLE_TH_ERRORS
 }
 
+// Element strides of the rows of t [.., .., .., D]: 0 where there is one alone.
+std::array<int64_t, 3> row_strides(const Tensor &t) {
+    std::array<int64_t, 3> st{0, 0, 0};
+    for (int i = 0; t.defined() && i < 3; ++i) st[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    return st;
+}
+
+// The rotation of rows: frequencies, the pairs of each axis, positions.
+struct Turn {
+    Tensor freq, pos;
+    std::array<int32_t, 3> pairs{0, 0, 0};
+    std::array<int64_t, 3> ps{0, 0, 0};   // of pos: axis, and the positions' own dimensions
+};
+
+// `sections` None or a tuple of whole numbers; positions of `shape`, behind an axis,
+// or for one axis alone.
+bool turn_ok(Turn &t, PyObject *sections, at::IntArrayRef shape, int64_t D) {
+    if (!t.freq.defined()) return !t.pos.defined() && sections == Py_None;
+    if (t.freq.scalar_type() != at::kFloat || t.freq.dim() != 1 || !t.freq.is_contiguous()) return false;
+    const int64_t total = t.freq.size(0);
+    int64_t axes = 1;
+    if (total > D / 2) return false;
+    if (sections == Py_None) {
+        t.pairs[0] = (int32_t)total;
+    } else {
+        if (!PyTuple_CheckExact(sections)) return false;
+        axes = PyTuple_GET_SIZE(sections);
+        if (axes < 1 || axes > 3) return false;
+        int64_t sum = 0;
+        for (int64_t i = 0; i < axes; ++i) {
+            PyObject *const o = PyTuple_GET_ITEM(sections, i);
+            if (!PyLong_CheckExact(o)) return false;
+            int overflow = 0;
+            const long long n = PyLong_AsLongLongAndOverflow(o, &overflow);
+            if (overflow || n < 0 || n > total) return false;
+            t.pairs[i] = (int32_t)n;
+            sum += n;
+        }
+        if (sum != total) return false;
+    }
+    if (!t.pos.defined()) return true;
+    const int64_t dims = (int64_t)shape.size(), at = t.pos.dim();
+    if (t.pos.scalar_type() != at::kInt || at < 1 || at > dims + 1) return false;
+    if (at == dims + 1 ? t.pos.size(0) != axes : axes != 1) return false;
+    const int64_t own = std::min(at, dims);   // trailing dimensions of `shape` that pos has
+    for (int64_t i = 0; i < own; ++i)
+        if (t.pos.size(at - own + i) != shape[dims - own + i]) return false;
+    for (int64_t i = 0; i < at; ++i) t.ps[dims + 1 - at + i] = t.pos.stride(i);
+    return true;
+}
+
+// q, k, pos, freq, sections, dtype, q_out, k_out, stream, back
+PyObject *rotate(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 10);
+    Turn t;
+    const Tensor q = a.tensor(), k = a.tensor(true);
+    t.pos = a.tensor(true), t.freq = a.tensor(true);
+    PyObject *const sections = a.next(), *const dtype = a.next();
+    Tensor qo = a.tensor(true), ko = a.tensor(true);
+    a.none();
+    const bool back = a.boolean();
+    if (!a.ok || q.dim() != 4 || dtype_of(q) < 0 || q.numel() == 0 || q.stride(3) != 1) Py_RETURN_NONE;
+    if (dtype != Py_None && !THPDtype_Check(dtype)) Py_RETURN_NONE;
+    const int64_t B = q.size(0), H = q.size(1), N = q.size(2), D = q.size(3);
+    const int64_t Hk = k.defined() && k.dim() == 4 ? k.size(1) : 0;
+    if (B > INT32_MAX || H > INT32_MAX || Hk > INT32_MAX || N > INT32_MAX || D > INT32_MAX) Py_RETURN_NONE;
+    if (k.defined() ? k.dim() != 4 || k.size(0) != B || k.size(2) != N || k.size(3) != D || k.stride(3) != 1 ||
+                          k.scalar_type() != q.scalar_type()
+                    : ko.defined())
+        Py_RETURN_NONE;
+    const at::ScalarType want = dtype != Py_None ? reinterpret_cast<THPDtype *>(dtype)->scalar_type
+                                : qo.defined()   ? qo.scalar_type()
+                                : ko.defined()   ? ko.scalar_type()
+                                                 : q.scalar_type();
+    if (want != at::kFloat && want != at::kBFloat16) Py_RETURN_NONE;
+    const auto fits = [&](const Tensor &o, const Tensor &x) {
+        return !o.defined() || (o.sizes() == x.sizes() && o.scalar_type() == want && o.stride(3) == 1);
+    };
+    if (!fits(qo, q) || !fits(ko, k) || !turn_ok(t, sections, {B, N}, D)) Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        const auto options = at::TensorOptions().dtype(want).device(a.device);
+        if (!qo.defined()) qo = at::empty(q.sizes(), options);
+        if (k.defined() && !ko.defined()) ko = at::empty(k.sizes(), options);
+        const auto qs = row_strides(q), ks = row_strides(k), qos = row_strides(qo), kos = row_strides(ko);
+        status = pi_attn_rotate(dtype_of(q), dtype_of(qo), B, H, Hk, N, D, back, q.data_ptr(), qs[0], qs[1], qs[2],
+                                ptr<void>(k), ks[0], ks[1], ks[2], ptr<int32_t>(t.pos), t.ps[0], t.ps[1], t.ps[2],
+                                ptr<float>(t.freq), t.pairs[0], t.pairs[1], t.pairs[2], qo.data_ptr(), qos[0], qos[1],
+                                qos[2], ptr<void>(ko), kos[0], kos[1], kos[2], stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, back ? "pi_attn_rotate_backward" : "pi_attn_rotate");
+    if (ko.defined()) return pack({qo, ko});
+    return PyTuple_Pack(2, pybind11::reinterpret_steal<pybind11::object>(THPVariable_Wrap(qo)).ptr(), Py_None);
+    END_HANDLE_TH_ERRORS
+}
+
+// A paged cache: pages [n, Hk, page, D], bytes [n, Hk, page], table [S, max], no empty extent.
+struct Paged {
+    Tensor k, v, ke, ve, table;
+    int64_t n, Hk, page, D, S, max;
+};
+
+bool paged_ok(Paged &g, at::ScalarType rows) {
+    if (g.k.dim() != 4 || g.k.numel() == 0 || !g.k.is_contiguous() || !g.v.is_contiguous()) return false;
+    const bool quantised = g.k.scalar_type() == at::kFloat8_e4m3fn;
+    if (g.v.scalar_type() != g.k.scalar_type() || g.v.sizes() != g.k.sizes()) return false;
+    if (!quantised && g.k.scalar_type() != rows) return false;
+    if (g.table.scalar_type() != at::kInt || g.table.dim() != 2 || !g.table.is_contiguous() || g.table.numel() == 0)
+        return false;
+    g.n = g.k.size(0), g.Hk = g.k.size(1), g.page = g.k.size(2), g.D = g.k.size(3);
+    g.S = g.table.size(0), g.max = g.table.size(1);
+    for (const int64_t x : {g.n, g.Hk, g.page, g.D, g.S, g.max})
+        if (x > INT32_MAX) return false;
+    if (g.ke.defined() != quantised || g.ve.defined() != quantised) return false;
+    const std::array<int64_t, 3> bytes{g.n, g.Hk, g.page};
+    return !quantised || (bytes_ok(g.ke, bytes) && bytes_ok(g.ve, bytes));
+}
+
+// k, v [S, Hk, n, D] of a paged cache's rows.
+bool paged_rows_ok(const Tensor &k, const Tensor &v, const Paged &g) {
+    return k.dim() == 4 && dtype_of(k) >= 0 && v.scalar_type() == k.scalar_type() && same_layout(k, v) &&
+           k.size(0) == g.S && k.size(1) == g.Hk && k.size(3) == g.D && k.stride(3) == 1 && k.size(2) <= INT32_MAX;
+}
+
+// k, v, k_pages, v_pages, table, start, count, k_exp, v_exp, freq, pos, sections, stream
+PyObject *paged_store(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 13);
+    Paged g;
+    Turn t;
+    const Tensor k = a.tensor(), v = a.tensor();
+    g.k = a.tensor(), g.v = a.tensor(), g.table = a.tensor();
+    const Tensor start = a.tensor(true), count = a.tensor(true);
+    g.ke = a.tensor(true), g.ve = a.tensor(true);
+    t.freq = a.tensor(true), t.pos = a.tensor(true);
+    PyObject *const sections = a.next();
+    a.none();
+    if (!a.ok || dtype_of(k) < 0 || !paged_ok(g, k.scalar_type()) || !paged_rows_ok(k, v, g) ||
+        !per_sequence(start, g.S) || !per_sequence(count, g.S) || !turn_ok(t, sections, {g.S, k.size(2)}, g.D))
+        Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        const auto ks = row_strides(k);
+        status = pi_attn_paged_store(dtype_of(k), g.S, g.Hk, g.D, k.size(2), g.n, g.page, g.max, k.data_ptr(),
+                                     v.data_ptr(), ks[0], ks[1], ks[2], ptr<int32_t>(start), ptr<int32_t>(count),
+                                     ptr<int32_t>(g.table), g.k.data_ptr(), g.v.data_ptr(), ptr<uint8_t>(g.ke),
+                                     ptr<uint8_t>(g.ve), ptr<float>(t.freq), t.pairs[0], t.pairs[1], t.pairs[2],
+                                     ptr<int32_t>(t.pos), t.ps[0], t.ps[1], t.ps[2], stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_paged_store");
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// k_pages, v_pages, table, n, start, count, k_exp, v_exp, dtype, k, v, stream
+PyObject *paged_load(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 12);
+    Paged g;
+    g.k = a.tensor(), g.v = a.tensor(), g.table = a.tensor();
+    const int32_t rows = a.integer();
+    const Tensor start = a.tensor(true), count = a.tensor(true);
+    g.ke = a.tensor(true), g.ve = a.tensor(true);
+    PyObject *const dtype = a.next();
+    Tensor k = a.tensor(true), v = a.tensor(true);
+    a.none();
+    if (!a.ok || rows < 1 || k.defined() != v.defined() || (dtype != Py_None && !THPDtype_Check(dtype))) Py_RETURN_NONE;
+    const at::ScalarType want = dtype != Py_None ? reinterpret_cast<THPDtype *>(dtype)->scalar_type
+                                : k.defined()    ? k.scalar_type()
+                                : g.k.scalar_type() == at::kFloat8_e4m3fn ? at::kBFloat16
+                                                                          : g.k.scalar_type();
+    if ((want != at::kFloat && want != at::kBFloat16) || !paged_ok(g, want) || !per_sequence(start, g.S) ||
+        !per_sequence(count, g.S))
+        Py_RETURN_NONE;
+    if (k.defined() && (k.scalar_type() != want || !paged_rows_ok(k, v, g) || k.size(2) != rows)) Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        if (!k.defined()) {
+            const std::array<int64_t, 4> shape{g.S, g.Hk, rows, g.D};
+            const auto options = at::TensorOptions().dtype(want).device(a.device);
+            k = at::empty(shape, options);
+            v = at::empty(shape, options);
+        }
+        const auto ks = row_strides(k);
+        status = pi_attn_paged_load(dtype_of(k), g.S, g.Hk, g.D, rows, g.n, g.page, g.max, g.k.data_ptr(),
+                                    g.v.data_ptr(), ptr<uint8_t>(g.ke), ptr<uint8_t>(g.ve), ptr<int32_t>(start),
+                                    ptr<int32_t>(count), ptr<int32_t>(g.table), k.data_ptr(), v.data_ptr(), ks[0], ks[1],
+                                    ks[2], stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_paged_load");
+    return pack({k, v});
+    END_HANDLE_TH_ERRORS
+}
+
+// len_in, q_new, k_new, v_new, k_pages, v_pages, table, gate, k, pi, k_exp, v_exp, freq, pos, sections, scale,
+// logit_clamp, len_out, out, lse, work, stream
+PyObject *decode_step_paged(PyObject *self, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 22);
+    Paged g;
+    Turn t;
+    const Tensor len_in = a.tensor(), q = a.tensor(), k = a.tensor(), v = a.tensor();
+    g.k = a.tensor(), g.v = a.tensor(), g.table = a.tensor();
+    const Tensor gate = a.tensor();
+    const int32_t kw = a.integer(), pi = a.integer();
+    g.ke = a.tensor(true), g.ve = a.tensor(true);
+    t.freq = a.tensor(true), t.pos = a.tensor(true);
+    PyObject *const sections = a.next();
+    if (!a.ok || dtype_of(q) < 0 || !paged_ok(g, q.scalar_type())) Py_RETURN_NONE;
+    const float scale = a.real(pi_attn_default_scale((int32_t)g.D)), clamp = a.real(NAN);
+    const Tensor len_out = a.tensor(true);
+    Tensor out = a.tensor(true);
+    const Tensor lse = a.tensor(true);
+    Tensor work = a.tensor(true);
+    a.none();
+    if (!a.ok || q.dim() != 3 || q.size(0) != g.S || q.size(2) != g.D || !q.is_contiguous() || q.numel() == 0 ||
+        q.size(1) > INT32_MAX || q.size(1) % g.Hk != 0)
+        Py_RETURN_NONE;
+    const int64_t H = q.size(1);
+    const std::array<int64_t, 3> key_rows{g.S, g.Hk, g.D};
+    for (const Tensor &x : {k, v})
+        if (x.scalar_type() != q.scalar_type() || x.sizes() != at::IntArrayRef(key_rows) || !x.is_contiguous())
+            Py_RETURN_NONE;
+    if (!per_sequence(len_in, g.S) || !per_sequence(len_out, g.S) || gate.scalar_type() != at::kFloat ||
+        !turn_ok(t, sections, {g.S}, g.D))
+        Py_RETURN_NONE;
+    int64_t gss, gsh;
+    if (gate.dim() == 1 && gate.size(0) == H) {
+        gss = 0;
+        gsh = gate.stride(0);
+    } else if (gate.dim() == 2 && gate.size(0) == g.S && gate.size(1) == H) {
+        gss = gate.stride(0);
+        gsh = gate.stride(1);
+    } else {
+        Py_RETURN_NONE;
+    }
+    if (out.defined() && (out.scalar_type() != q.scalar_type() || out.sizes() != q.sizes() || !out.is_contiguous()))
+        Py_RETURN_NONE;
+    if (lse.defined() && !is_f32(lse, {g.S, H})) Py_RETURN_NONE;
+    const int64_t need = pi_attn_paged_workspace(dtype_of(q), g.S, H, g.Hk, g.D, g.page, g.max, kw);
+    if (need < 0) Py_RETURN_NONE;
+    if (work.defined() && (work.scalar_type() != at::kFloat || !work.is_contiguous() || work.numel() < need))
+        Py_RETURN_NONE;
+    int status;
+    {
+        pybind11::gil_scoped_release no_gil;
+        const c10::DeviceGuard on(a.device);
+        if (!out.defined()) out = at::empty(q.sizes(), at::TensorOptions().dtype(q.scalar_type()).device(a.device));
+        if (!work.defined() && need > 0) work = at::empty({need}, at::TensorOptions().dtype(at::kFloat).device(a.device));
+        status = pi_attn_decode_step_paged(
+            dtype_of(q), g.S, H, g.Hk, g.D, g.n, g.page, g.max, kw, pi, ptr<int32_t>(len_in), ptr<int32_t>(len_out),
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), ptr<int32_t>(g.table), g.k.data_ptr(), g.v.data_ptr(),
+            ptr<uint8_t>(g.ke), ptr<uint8_t>(g.ve), ptr<float>(t.freq), t.pairs[0], t.pairs[1], t.pairs[2],
+            ptr<int32_t>(t.pos), t.ps[0], t.ps[1], ptr<float>(gate), gss, gsh, scale, clamp, out.data_ptr(),
+            ptr<float>(lse), ptr<float>(work), stream_of(a.device));
+    }
+    if (status != PI_ATTN_OK) return refused(self, status, "pi_attn_decode_step_paged");
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction fast(F f) {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -573,6 +842,10 @@ PyMethodDef methods[] = {{"forward", fast(forward), METH_FASTCALL, nullptr},
                          {"cache_load", fast(cache_load), METH_FASTCALL, nullptr},
                          {"decode_step_e4m3", fast(decode_step_e4m3), METH_FASTCALL, nullptr},
                          {"decode_step_prefix", fast(decode_step_prefix), METH_FASTCALL, nullptr},
+                         {"rotate", fast(rotate), METH_FASTCALL, nullptr},
+                         {"paged_store", fast(paged_store), METH_FASTCALL, nullptr},
+                         {"paged_load", fast(paged_load), METH_FASTCALL, nullptr},
+                         {"decode_step_paged", fast(decode_step_paged), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,75 @@
+// paged.h -- parameters and launches of the rotary positions, of the paged
+// caches' rows and of the decode step over them.
+#pragma once
+
+#include "cached.h"
+#include "rotary.h"
+
+namespace pi_attn {
+
+// Rows of q [B][H][N][D] and k [B][Hk][N][D] turned, forward or back.
+struct RotateParams {
+    int B, H, Hk, N, D;
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t qsb, qsh, qsn, ksb, ksh, ksn;          // element strides of q and k,
+    int64_t oqsb, oqsh, oqsn, oksb, oksh, oksn;    // of their results
+    Rotary r;
+    bool back;                      // the transpose: by the angle's negative
+    uint32_t rows;                  // B * N, at least 1
+    Divisor by_n;
+    int per, splits;                // heads of a wavefront, and wavefronts for all of them; set by the launch
+    Divisor by_splits;
+};
+
+// A paged cache: position j of sequence s is row j mod page of page
+// table[s][j / page]; an entry that names no page has no rows.
+struct Pages {
+    int n_pages, page, max_pages;   // pages in all, rows of one, entries of a sequence
+    Divisor by_page;
+    const int32_t *table;           // [S][max_pages]
+    void *k, *v;                    // [n_pages][Hk][page][D], rows or codes
+    uint8_t *k_exp, *v_exp;         // [n_pages][Hk][page]; nullptr: not quantised
+};
+
+// Rows of k and v [S][Hk][n][D] into or out of a paged cache.
+struct PagedRowsParams {
+    int S, Hk, n, D;
+    void *k, *v;                    // read by a store, written by a load
+    int64_t sb, sh, sn;
+    const int32_t *start, *count;   // [S], or nullptr: 0, n
+    Pages pages;
+    Rotary r;                       // of the keys stored
+    uint32_t rows;                  // S * n, at least 1
+    Divisor by_n;
+    int per, splits;                // as of RotateParams
+    Divisor by_splits;
+};
+
+// A decode step over a paged cache: H query heads, H / Hk to a key head.
+struct PagedStepParams {
+    int S, H, Hk, D, k, pi;
+    const int32_t *len_in;
+    int32_t *len_out;               // nullptr: not written
+    const void *q_new, *k_new, *v_new;   // [S][H][D], [S][Hk][D]
+    Pages pages;
+    Rotary r;                       // of q_new and k_new
+    const float *gate;
+    int64_t gss, gsh;
+    float scale, clamp;
+    void *out;                      // [S][H][D]
+    float *lse;                     // [S][H] or nullptr
+    // Ranges of `range` window rows that leave parts (parts = 0: not split): for
+    // part x at[x][s * H + h] the weighted values [D], then (max, sum) in log2 units.
+    float *part_o, *part_ml;
+    int range, parts;
+};
+
+hipError_t launch_rotate(const RotateParams &p, bool bf16_in, bool bf16_out, hipStream_t stream);
+hipError_t launch_paged_rows(const PagedRowsParams &p, bool store, bool bf16, hipStream_t stream);
+
+// The sizes of the parts, by the problem's sizes alone; then the step.
+void plan_decode_paged(PagedStepParams &p, bool bf16);
+hipError_t launch_decode_paged(const PagedStepParams &p, bool bf16, hipStream_t stream);
+
+}  // namespace pi_attn

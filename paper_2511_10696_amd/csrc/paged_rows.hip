@@ -1,0 +1,216 @@
+// paged_rows.hip -- rows of keys and values into and out of a paged cache:
+// float32 or bf16 rows, pages in the same type or quantised (e4m3.h), D = 64 or
+// 128.  A store turns the keys by their positions on the way (rotary.h), in fp32,
+// with one rounding to what the page holds.
+//
+// A wavefront takes a few rows of one sequence (as many as one load instruction
+// covers), looks their pages up and forms their cosines and sines once, and walks
+// over the heads.
+//
+// What bounds it: HBM, rows read and written once.
+#include <algorithm>
+
+#include "e4m3.h"
+#include "half_rows.h"
+#include "paged.h"
+#include "pi_common.h"
+
+namespace pi_attn {
+
+namespace {
+
+constexpr int WAVES = 4;
+constexpr int U = 2;   // heads whose loads are in flight together, keys and values
+
+// What a lane does for its row, all heads alike.
+struct Place {
+    bool there;       // the row has a place in the cache
+    uint32_t s, i;    // sequence and row of k and v
+    int at;           // its position
+    int64_t first;    // cache row of head 0; head h's is h * page further on
+};
+
+template <int RPI>
+__device__ inline bool place(const PagedRowsParams &p, uint32_t tile, int rg, Place &a) {
+    const uint32_t r = tile * RPI + rg;
+    if (r >= p.rows) return false;
+    a.s = p.by_n.div(r);
+    a.i = r - a.s * p.n;
+    const int64_t at = (int64_t)a.i + (p.start ? p.start[a.s] : 0);
+    const Pages &g = p.pages;
+    a.there = at >= 0 && at < (int64_t)g.page * g.max_pages && (!p.count || (int)a.i < p.count[a.s]);
+    a.at = a.there ? (int)at : 0;
+    const uint32_t slot = g.by_page.div(a.at);
+    const int entry = a.there ? g.table[(int64_t)a.s * g.max_pages + slot] : -1;
+    a.there = a.there && entry >= 0 && entry < g.n_pages;
+    a.first = (int64_t)(a.there ? entry : 0) * p.Hk * g.page + (a.at - slot * g.page);
+    return true;
+}
+
+template <typename T, bool QUANT, int D, bool ONCE>
+__global__ __launch_bounds__(64 * WAVES) void paged_store_kernel(PagedRowsParams p) {
+    using R = HalfRow<T, D>;
+    constexpr int EPL = R::EPL;
+    const int lane = __lane_id(), sub = lane % R::LPR, rg = lane / R::LPR;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + (threadIdx.x >> 6));
+    const uint32_t tile = p.by_splits.div(wave);
+    Place a;
+    if (!place<R::RPI>(p, tile, rg, a)) return;
+    if (!a.there) return;   // a row's lanes alike
+    const int h0 = (int)(wave - tile * p.splits) * p.per, h1 = min(h0 + p.per, p.Hk);
+    const int64_t from = a.s * p.sb + a.i * p.sn + sub * EPL;
+    const T *k = (const T *)p.k + from, *v = (const T *)p.v + from;
+
+    float2 cs[EPL];
+    bool turned[EPL];
+    if (p.r.freq) {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) {
+            const int i = sub * EPL + e;
+            cs[e] = cos_sin_of(p.r, i, a.s, a.i, a.at);
+            turned[e] = i < p.r.pairs;
+        }
+    }
+    const Pages &g = p.pages;
+    // A row's halves into head h's pages, as these hold them.
+    auto put = [&](const Piece<T, EPL> &lo, const Piece<T, EPL> &hi, bool turns, int h, void *pages, uint8_t *exps)
+        __attribute__((always_inline)) {
+        const int64_t row = a.first + (int64_t)h * g.page;
+        float x[EPL], y[EPL];
+        if (QUANT || turns) {
+            widen<T, EPL>(lo, x);
+            widen<T, EPL>(hi, y);
+        }
+        if (turns) {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) turn(x[e], y[e], cs[e], turned[e]);
+        }
+        if constexpr (QUANT) {
+            unsigned m = 0;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) m = max(m, max(finite_bits(x[e]), finite_bits(y[e])));
+            const unsigned byte = e4m3_byte(row_max<R::LPR>(m));
+            const float inv = e4m3_inverse(byte);
+            Piece<uint8_t, EPL> cl, ch;
+#pragma unroll
+            for (int i = 0; i < EPL / 4; ++i) {
+                cl.w[i] = e4m3_pack4(x + 4 * i, inv);
+                ch.w[i] = e4m3_pack4(y + 4 * i, inv);
+            }
+            uint8_t *to = (uint8_t *)pages + row * D + sub * EPL;
+            store_piece<uint8_t, EPL, ONCE>(cl, to);
+            store_piece<uint8_t, EPL, ONCE>(ch, to + D / 2);
+            if (sub == 0) exps[row] = (uint8_t)byte;
+        } else {
+            T *to = (T *)pages + row * D + sub * EPL;
+            store_piece<T, EPL, ONCE>(turns ? narrowed<T, EPL>(x) : lo, to);
+            store_piece<T, EPL, ONCE>(turns ? narrowed<T, EPL>(y) : hi, to + D / 2);
+        }
+    };
+    for (int h = h0; h < h1; h += U) {
+        Piece<T, EPL> kl[U], kh[U], vl[U], vh[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t x = min(h + u, h1 - 1) * p.sh;
+            kl[u] = load_piece<T, EPL, ONCE>(k + x);
+            kh[u] = load_piece<T, EPL, ONCE>(k + x + D / 2);
+            vl[u] = load_piece<T, EPL, ONCE>(v + x);
+            vh[u] = load_piece<T, EPL, ONCE>(v + x + D / 2);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (h + u >= h1) break;
+            put(kl[u], kh[u], p.r.freq != nullptr, h + u, g.k, g.k_exp);
+            put(vl[u], vh[u], false, h + u, g.v, g.v_exp);
+        }
+    }
+}
+
+template <typename T, bool QUANT, int D, bool ONCE>
+__global__ __launch_bounds__(64 * WAVES) void paged_load_kernel(PagedRowsParams p) {
+    using R = HalfRow<T, D>;
+    constexpr int EPL = R::EPL;
+    using ST = typename std::conditional<QUANT, uint8_t, T>::type;   // what the pages hold
+    const int lane = __lane_id(), sub = lane % R::LPR, rg = lane / R::LPR;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + (threadIdx.x >> 6));
+    const uint32_t tile = p.by_splits.div(wave);
+    Place a;
+    if (!place<R::RPI>(p, tile, rg, a)) return;
+    const int h0 = (int)(wave - tile * p.splits) * p.per, h1 = min(h0 + p.per, p.Hk);
+    const int64_t to = a.s * p.sb + a.i * p.sn + sub * EPL;
+    T *k = (T *)p.k + to, *v = (T *)p.v + to;
+    const Pages &g = p.pages;
+    const ST *kp = (const ST *)g.k + sub * EPL, *vp = (const ST *)g.v + sub * EPL;
+    auto out = [&](const Piece<ST, EPL> &x, unsigned byte, T *y) __attribute__((always_inline)) {
+        if constexpr (QUANT) {
+            const float scale = e4m3_scale(byte);
+            float f[EPL];
+#pragma unroll
+            for (int i = 0; i < EPL / 4; ++i) e4m3_unpack4(x.w[i], f + 4 * i);
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) f[e] *= scale;
+            store_piece<T, EPL, ONCE>(narrowed<T, EPL>(f), y);
+        } else {
+            store_piece<T, EPL, ONCE>(x, y);
+        }
+    };
+    for (int h = h0; h < h1; h += U) {
+        Piece<ST, EPL> x[U][4];
+        unsigned kb[U], vb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            kb[u] = vb[u] = 127;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[u][j] = Piece<ST, EPL>{};   // absent rows: zeros, in codes too
+            if (a.there) {
+                const int64_t row = a.first + (int64_t)min(h + u, h1 - 1) * g.page;
+                x[u][0] = load_piece<ST, EPL, false>(kp + row * D);
+                x[u][1] = load_piece<ST, EPL, false>(kp + row * D + D / 2);
+                x[u][2] = load_piece<ST, EPL, false>(vp + row * D);
+                x[u][3] = load_piece<ST, EPL, false>(vp + row * D + D / 2);
+                if constexpr (QUANT) {
+                    kb[u] = g.k_exp[row];
+                    vb[u] = g.v_exp[row];
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (h + u >= h1) break;
+            const int64_t y = (h + u) * p.sh;
+            out(x[u][0], kb[u], k + y);
+            out(x[u][1], kb[u], k + y + D / 2);
+            out(x[u][2], vb[u], v + y);
+            out(x[u][3], vb[u], v + y + D / 2);
+        }
+    }
+}
+
+template <typename T, bool QUANT, int D>
+hipError_t launch_d(PagedRowsParams p, bool store, hipStream_t stream) {
+    using R = HalfRow<T, D>;
+    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI;
+    p.splits = (int)std::clamp<int64_t>(8192 / tiles, 1, (p.Hk + U - 1) / U);
+    p.per = ((p.Hk + p.splits - 1) / p.splits + U - 1) / U * U;
+    p.splits = (p.Hk + p.per - 1) / p.per;
+    p.by_splits = Divisor(p.splits);
+    const int64_t groups = (tiles * p.splits + WAVES - 1) / WAVES;
+    if (groups >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
+    return launch_kernel(store ? paged_store_kernel<T, QUANT, D, false> : paged_load_kernel<T, QUANT, D, false>,
+                         dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
+}
+
+template <typename T>
+hipError_t launch_t(const PagedRowsParams &p, bool store, hipStream_t stream) {
+    if (p.pages.k_exp)
+        return p.D == 64 ? launch_d<T, true, 64>(p, store, stream) : launch_d<T, true, 128>(p, store, stream);
+    return p.D == 64 ? launch_d<T, false, 64>(p, store, stream) : launch_d<T, false, 128>(p, store, stream);
+}
+
+}  // namespace
+
+hipError_t launch_paged_rows(const PagedRowsParams &p, bool store, bool bf16, hipStream_t stream) {
+    return bf16 ? launch_t<__bf16>(p, store, stream) : launch_t<float>(p, store, stream);
+}
+
+}  // namespace pi_attn

@@ -1,0 +1,47 @@
+// rotary.h -- rotary positions: pair i < P of a row, its elements i and i + D/2,
+// is turned by the angle pos_a * freq_i, a the axis that the pair belongs to
+// (one, or up to three: time, height and width); pairs from P on stay as they
+// are.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace pi_attn {
+
+// pos == nullptr: the position of a row in its sequence, on every axis.
+struct Rotary {
+    const float *freq;              // [pairs], radians a position; nullptr: no rotation
+    int pairs, end0, end1;          // axis 0 has pairs [0, end0), axis 1 [end0, end1), axis 2 the rest
+    const int32_t *pos;
+    int64_t psa, psb, psn;          // its element strides: axis, sequence, row
+};
+
+// cos and sin of pos * freq.  The angle is formed in turns and in 64 bits, where
+// |pos| < 2^31 leaves an error below 2^-24 of a turn for |freq| <= 1 (2^-34 up to a
+// million positions); in 32 bits a position of 2^20 would be off by a hundredth
+// of a turn.
+__device__ inline float2 cos_sin(int pos, float freq) {
+    constexpr double kTurns = 0.15915494309189535;   // 1 / (2 pi)
+    const double turns = (double)pos * ((double)freq * kTurns);
+    const float x = 2.0f * (float)(turns - __builtin_rint(turns));
+    float s, c;
+    sincospif(x, &s, &c);
+    return make_float2(c, s);
+}
+
+// Of pair i at row n of sequence b, which is position `at` of the sequence.
+__device__ inline float2 cos_sin_of(const Rotary &r, int i, int64_t b, int64_t n, int at) {
+    if (i >= r.pairs) return make_float2(1.0f, 0.0f);
+    const int axis = i < r.end0 ? 0 : i < r.end1 ? 1 : 2;
+    return cos_sin(r.pos ? r.pos[axis * r.psa + b * r.psb + n * r.psn] : at, r.freq[i]);
+}
+
+// A pair (a, b) turned; pairs from r.pairs on are not touched, whatever they hold.
+__device__ inline void turn(float &a, float &b, float2 cs, bool turned) {
+    const float x = a * cs.x - b * cs.y, y = a * cs.y + b * cs.x;
+    a = turned ? x : a;
+    b = turned ? y : b;
+}
+
+}  // namespace pi_attn
