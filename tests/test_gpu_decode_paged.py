@@ -1,0 +1,337 @@
+"""The decode step over paged caches against attention in 64 bits over the rows as stored, within bounds
+derived in paged_ref.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_10696_amd as pa
+from tests.cached_ref import f64, quantise
+from tests.paged_ref import Cache, PagedStep, frequencies, rounded_tol, turned
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+
+
+def i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def new_rows(S, H, Hk, D, dtype, seed, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    q = (size * torch.randn(S, H, D, generator=g)).to(dtype).cuda()
+    k, v = (torch.randn(S, Hk, D, generator=g).to(dtype).cuda() for _ in range(2))
+    gate = (torch.rand(S, H, generator=g) * 2 - 1).cuda()
+    return q, k, v, gate
+
+
+def run(cache, lens, q, k, v, gate, kw, pi, clamp=0.0, freq=None, sections=None, pos=None, **more):
+    """A step, checked in full: outputs, lse, lengths, the new rows and everything else of the cache."""
+    before = [t.clone() for t in cache.tensors()]
+    S, H, D = q.shape
+    len_in, len_out = i32(*lens), i32(*[-9] * S)
+    lse = torch.full((S, H), 5.0, device="cuda")
+    out = pa.pi_attn_decode_step_paged(len_in, q, k, v, cache.k, cache.v, cache.table, gate, kw, pi, **cache.args(), freq=freq,
+                                       pos=pos, sections=sections, logit_clamp=clamp, len_out=len_out, lse=lse, **more)
+    quantised = cache.k_exp is not None
+    kt, tol = f64(k), np.zeros(k.shape)
+    if freq is not None:
+        sections = sections or (len(freq),)
+        at = np.array([lens] * len(sections)) if pos is None else np.asarray(pos.cpu()).reshape(len(sections), S)
+        kt, tol = turned(kt, at[:, :, None], freq, sections)
+    keys, vals = cache.values()
+    for s, t in enumerate(lens):
+        e = cache.entry(s, t)
+        assert int(len_out[s]) == (t + 1 if e >= 0 else t)
+        if e < 0:
+            continue
+        r = t % cache.page
+        if quantised:
+            scale = np.ldexp(1.0, cache.k_exp[e, :, r].cpu().numpy().astype(int) - 127)[:, None]
+            bound = tol[s] + np.maximum(2.0 ** -4 * np.abs(kt[s]) + tol[s], 2.0 ** -10 * scale)
+            c, b = quantise(v[s])
+            assert np.array_equal(vals[e, :, r], c * np.ldexp(1.0, b.astype(int) - 127)[:, None])
+        else:
+            bound = rounded_tol(kt[s], tol[s], q.dtype) if freq is not None else 0 * kt[s]
+            assert np.array_equal(vals[e, :, r], f64(v[s]))
+        assert (np.abs(keys[e, :, r] - kt[s]) <= bound).all()
+        for x, y in zip(cache.tensors(), before):
+            y[e, :, r] = x[e, :, r] if x.dtype != cache.k.dtype or not quantised else y[e, :, r]
+            if quantised and x.dtype == cache.k.dtype:
+                y.view(torch.uint8)[e, :, r] = x.view(torch.uint8)[e, :, r]
+    for x, y in zip(cache.tensors(), before):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    want = PagedStep(cache, lens, q, gate.cpu() if gate.dim() == 2 else gate.cpu().expand(S, H), kw, pi, clamp, freq, sections, pos,
+                     two_terms=q.dtype == BF)
+    want.check(out, lse)
+    return out, lse
+
+
+CASES = [
+    # H, Hk, D, page, max_pages, dtype, quantised, k, pi, clamp, lengths
+    (1, 1, 64, 1, 40, F, False, 5, 9, 0.0, [0, 1, 5, 39]),
+    (4, 4, 64, 5, 13, F, False, 20, 33, 0.0, [0, 1, 4, 5, 21, 64]),
+    (4, 4, 128, 16, 8, BF, False, 100, 0, 0.0, [0, 15, 16, 17, 127]),
+    (6, 3, 128, 7, 30, BF, False, 64, 65, 20.0, [0, 63, 64, 65, 66, 209]),
+    (9, 3, 64, 16, 10, BF, False, 33, 60, 0.0, [1, 34, 60, 61, 159]),
+    (8, 2, 128, 32, 5, BF, False, 1000, 0, 0.0, [0, 31, 159]),
+    (10, 2, 64, 64, 3, F, False, 70, 100, 2.0, [0, 99, 100, 191]),
+    (16, 2, 128, 3, 50, BF, False, 149, 150, 0.0, [2, 148, 149]),
+    (34, 2, 64, 16, 9, BF, False, 200, 0, 0.0, [0, 30, 143]),
+    (5, 5, 64, 16, 9, BF, True, 40, 77, 0.0, [0, 40, 77, 143]),
+    (8, 2, 128, 16, 9, BF, True, 400, 0, 0.0, [1, 143]),
+    (16, 1, 64, 11, 13, F, True, 60, 61, 20.0, [0, 61, 142]),
+    (40, 1, 128, 16, 5, F, False, 79, 0, 0.0, [3, 79]),
+    (32, 2, 64, 5, 30, BF, True, 0, 5, 0.0, [0, 4, 5, 149]),
+]
+IDS = [f"{c[0]}over{c[1]}x{c[2]}-p{c[3]}-{'f32' if c[5] == F else 'bf16'}{'-e4m3' if c[6] else ''}-k{c[7]}" for c in CASES]
+
+
+def make(case, seed=1, per_sequence=True):
+    H, Hk, D, page, max_pages, dt, quantised, kw, pi, clamp, lens = case
+    cache = Cache(len(lens), Hk, D, page, max_pages, dt, quantised, seed, extra=1.0)
+    return cache, lens, *new_rows(len(lens), H, Hk, D, dt, seed + 1), kw, pi, clamp
+
+
+@pytest.mark.parametrize("turns", [False, True])
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_step(device, case, turns):
+    cache, lens, q, k, v, gate, kw, pi, clamp = make(case)
+    D = q.shape[2]
+    run(cache, lens, q, k, v, gate, kw, pi, clamp, freq=frequencies(D // 2).cuda() if turns else None)
+
+
+@pytest.mark.parametrize("case", CASES[1:12], ids=IDS[1:12])
+def test_pages_given_back(device, case):
+    """Pages behind the window, inside it, and the partner's, are gone for some of the sequences; what lies in page 0 and in the
+    rows past the lengths is NaN."""
+    cache, lens, q, k, v, gate, kw, pi, clamp = make(case, 5)
+    nan = float("nan")
+    for s, t in enumerate(lens):
+        for x in range(cache.max_pages):
+            if x != t // cache.page and (x + s) % 3 == 0:
+                cache.table[s, x] = (-1, cache.k.shape[0], 2 ** 31 - 1)[x % 3]
+    held = {cache.entry(s, j) for s, t in enumerate(lens) for j in range(t + 1)}
+    for e in range(cache.k.shape[0]):
+        if e not in held:
+            for x in (cache.k, cache.v):
+                if cache.k_exp is None:
+                    x[e] = nan
+                else:
+                    x.view(torch.uint8)[e] = 0x7f
+            for x in (cache.k_exp, cache.v_exp):
+                if x is not None:
+                    x[e] = 255
+    for s, t in enumerate(lens):
+        e, r = cache.entry(s, t), t % cache.page
+        for x in (cache.k, cache.v):
+            if cache.k_exp is None:
+                x[e, :, r:] = nan
+            else:
+                x.view(torch.uint8)[e, :, r:] = 0x7f
+    out, _ = run_with_nan(cache, lens, q, k, v, gate, kw, pi, clamp)
+    assert torch.isfinite(out).all()
+
+
+def run_with_nan(cache, lens, q, k, v, gate, kw, pi, clamp):
+    """As run(), of a cache that holds NaN where nothing is to be read."""
+    S, H, D = q.shape
+    lse = torch.empty(S, H, device="cuda")
+    out = pa.pi_attn_decode_step_paged(i32(*lens), q, k, v, cache.k, cache.v, cache.table, gate, kw, pi, **cache.args(),
+                                       logit_clamp=clamp, lse=lse)
+    PagedStep(cache, lens, q, gate.cpu(), kw, pi, clamp, two_terms=q.dtype == BF).check(out, lse)
+    return out, lse
+
+
+@pytest.mark.parametrize("quantised", [False, True])
+def test_lengths_without_a_place(device, quantised):
+    """Negative, past the table's reach, in a page that is not there: NaN, nothing stored, the length kept; others unharmed."""
+    cache = Cache(6, 2, 64, 8, 5, BF, quantised, 1)
+    cache.table[3, 2] = -1
+    cache.table[4, 0] = cache.k.shape[0]
+    lens = [-1, 40, 2 ** 31 - 1, 17, 0, 39]
+    run(cache, lens, *new_rows(6, 4, 2, 64, BF, 2), 20, 30)
+
+
+LONG = [
+    # H, Hk, D, page, rows, dtype, quantised, k, pi, clamp, lengths: windows split over work-groups
+    (8, 8, 128, 16, 5000, BF, False, 4999, 0, 0.0, [4990, 7, 1025]),
+    (8, 2, 64, 64, 9000, BF, False, 3000, 5000, 0.0, [8999, 0, 256, 3001]),
+    (4, 1, 128, 5, 4000, F, False, 4000, 0, 20.0, [3999, 257]),
+    (16, 2, 128, 128, 9000, BF, True, 9000, 0, 0.0, [8191, 8192]),
+    (3, 3, 64, 16, 3000, F, True, 2500, 2700, 0.0, [2999, 2700, 1]),
+    (33, 1, 64, 16, 3000, BF, False, 2900, 2901, 0.0, [2999, 2700]),
+]
+
+
+@pytest.mark.parametrize("turns", [False, True])
+@pytest.mark.parametrize("case", LONG, ids=[f"{c[0]}over{c[1]}x{c[2]}-{c[4]}" for c in LONG])
+def test_long_windows(device, case, turns):
+    H, Hk, D, page, n, dt, quantised, kw, pi, clamp, lens = case
+    S, max_pages = len(lens), -(-n // page)
+    assert pa.pi_attn_paged_workspace(dt, S, H, Hk, D, page, max_pages, kw) > 0
+    cache = Cache(S, Hk, D, page, max_pages, dt, quantised, 1)
+    cache.table[0, 3:5] = -1
+    q, k, v, gate = new_rows(S, H, Hk, D, dt, 2, size=2.0)
+    run(cache, lens, q, k, v, gate, kw, pi, clamp, freq=frequencies(D // 2).cuda() if turns else None)
+
+
+@pytest.mark.parametrize("quantised", [False, True])
+def test_long_windows_with_lengths_without_a_place(device, quantised):
+    cache = Cache(4, 1, 64, 16, 200, BF, quantised, 1)
+    cache.table[1, 100] = -1
+    lens = [-5, 1600, 3200, 3199]
+    assert pa.pi_attn_paged_workspace(BF, 4, 2, 1, 64, 16, 200, 3000) > 0
+    run(cache, lens, *new_rows(4, 2, 1, 64, BF, 2), 3000, 0)
+
+
+@pytest.mark.parametrize("sections,given", [((32,), True), ((12, 10, 10), True), ((12, 10, 10), False), ((7, 3), True), ((5,), False)])
+def test_positions(device, sections, given):
+    """Positions of one to three axes, given or the lengths; some pairs not turned."""
+    S, lens = 3, [0, 17, 63]
+    cache = Cache(S, 2, 64, 16, 4, F, False, 1)
+    pos = torch.randint(0, 100000, (len(sections), S), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda() if given else None
+    run(cache, lens, *new_rows(S, 4, 2, 64, F, 2), 30, 40, freq=frequencies(sum(sections)).cuda(), sections=sections, pos=pos)
+
+
+def test_as_the_contiguous_step(device):
+    """Pages that follow one another hold a contiguous cache: the same as pi_attn_decode_step within both steps' roundings."""
+    S, H, D, cap = 4, 3, 128, 96
+    lens = [0, 31, 32, 95]
+    cache = Cache(S, H, D, 32, 3, F, False, 1, spare=0)
+    cache.table.copy_(torch.arange(S * 3, dtype=torch.int32).view(S, 3))
+    kc, vc = (x.view(S, 3, H, 32, D).transpose(1, 2).reshape(S, H, cap, D).contiguous() for x in (cache.k, cache.v))
+    q, k, v, gate = new_rows(S, H, H, D, F, 2)
+    out, _ = run(cache, lens, q, k, v, gate, 40, 50)
+    want = pa.pi_attn_decode_step(i32(*lens), q, k, v, kc, vc, gate, 40, 50)
+    tol = PagedStep(cache, lens, q, gate.cpu(), 40, 50).out_tol
+    assert (np.abs(f64(out) - f64(want)) <= 2 * tol).all()
+
+
+def test_one_key_returns_its_value(device):
+    """An empty window: the new row's value, bit by bit."""
+    cache = Cache(2, 2, 64, 4, 2, BF, False, 1)
+    q, k, v, gate = new_rows(2, 4, 2, 64, BF, 2)
+    out, _ = run(cache, [0, 5], q, k, v, gate, 0, 0)
+    assert torch.equal(out, v.repeat_interleave(2, 1))
+
+
+def test_large_logits_and_masks_of_rows(device):
+    """Logits of hundreds; then a window whose pages are all gone but for the new row's."""
+    cache = Cache(2, 2, 128, 16, 8, BF, False, 1, extra=4.0)
+    run(cache, [100, 127], *new_rows(2, 8, 2, 128, BF, 2, size=60.0), 90, 95)
+    cache = Cache(2, 2, 128, 16, 8, BF, False, 1)
+    cache.table[:, :6] = -1
+    run(cache, [96, 112], *new_rows(2, 8, 2, 128, BF, 2), 90, 95)
+
+
+def test_nan_reaches_its_heads_alone(device):
+    """A NaN in a key row in the window: its key head's queries are NaN, others are not."""
+    for kw in (40, 2000):
+        cache = Cache(1, 2, 64, 16, 150 if kw > 100 else 4, BF, False, 1)
+        t = 16 * cache.max_pages - 1
+        e = cache.entry(0, t - 3)
+        cache.k[e, 1, (t - 3) % 16, 5] = float("nan")
+        q, k, v, gate = new_rows(1, 6, 2, 64, BF, 2)
+        out = pa.pi_attn_decode_step_paged(i32(t), q, k, v, cache.k, cache.v, cache.table, gate, kw, 0)
+        assert torch.isfinite(out[:, :3]).all() and torch.isnan(out[:, 3:]).all()
+
+
+def test_same_bits_and_own_workspace(device):
+    cache = Cache(2, 2, 128, 16, 200, BF, False, 1)
+    q, k, v, gate = new_rows(2, 8, 2, 128, BF, 2)
+    args = (i32(3000, 1700), q, k, v, cache.k, cache.v, cache.table, gate, 3100, 0)
+    need = pa.pi_attn_paged_workspace(BF, 2, 8, 2, 128, 16, 200, 3100)
+    work = torch.full((need + 8,), float("nan"), device="cuda")
+    out = pa.pi_attn_decode_step_paged(*args)
+    for _ in range(3):
+        assert torch.equal(out, pa.pi_attn_decode_step_paged(*args, work=work))
+    assert torch.isnan(work[need:]).all()
+    with pytest.raises(ValueError):
+        pa.pi_attn_decode_step_paged(*args, work=work[:need - 1])
+
+
+def test_on_a_given_stream_and_python_path(device, monkeypatch):
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(pa, "_native", pa._PythonOnly)
+        for given in (False, True):
+            cache = Cache(3, 2, 64, 16, 100, BF, False, 1)
+            q, k, v, gate = new_rows(3, 6, 2, 64, BF, 2)
+            st = torch.cuda.Stream() if given else None
+            if st:
+                st.wait_stream(torch.cuda.current_stream())
+            lse, len_out = torch.empty(3, 6, device="cuda"), i32(0, 0, 0)
+            out = pa.pi_attn_decode_step_paged(i32(5, 1500, 99), q, k, v, cache.k, cache.v, cache.table, gate[0], 1400, 1450,
+                                               freq=frequencies(32).cuda(), pos=i32(1, 2, 3), sections=(32,), logit_clamp=30.0,
+                                               lse=lse, len_out=len_out, stream=st)
+            torch.cuda.synchronize()
+            got.append((out, lse, len_out, cache.k, cache.v))
+    for g in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], g))
+
+
+def test_two_graphs_of_steps(device):
+    """Two captured graphs of split steps, each with its workspace, replayed in turn with eager steps between them."""
+    freq = frequencies(64).cuda()
+
+    def problem(seed):
+        cache = Cache(2, 2, 128, 16, 200, BF, False, seed)
+        q, k, v, gate = new_rows(2, 8, 2, 128, BF, seed + 1)
+        work = torch.empty(pa.pi_attn_paged_workspace(BF, 2, 8, 2, 128, 16, 200, 3100), device="cuda")
+        return cache, q, k, v, gate, i32(3000, 1200), i32(0, 0), torch.empty_like(q), work
+
+    def one(p):
+        cache, q, k, v, gate, a, b, out, work = p
+        pa.pi_attn_decode_step_paged(a, q, k, v, cache.k, cache.v, cache.table, gate, 3100, 0, freq=freq, len_out=b, out=out, work=work)
+        pa.pi_attn_decode_step_paged(b, q, k, v, cache.k, cache.v, cache.table, gate, 3100, 0, freq=freq, len_out=a, out=out, work=work)
+
+    eager, graphs = [problem(s) for s in (1, 5)], [problem(s) for s in (1, 5)]
+    captured = []
+    one(problem(9))
+    torch.cuda.synchronize()
+    for p in graphs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            one(p)
+        captured.append(g)
+    for step in range(4):
+        for p, g, e in zip(graphs, captured, eager):
+            g.replay()
+            one(e)
+        torch.cuda.synchronize()
+        for p, e in zip(graphs, eager):
+            for i in (0, 5, 6, 7):
+                if i:
+                    assert torch.equal(p[i], e[i]), (step, i)
+            assert torch.equal(p[0].k, e[0].k) and torch.equal(p[0].v, e[0].v)
+    assert graphs[0][5].tolist() == [3008, 1208]
+
+
+def test_refusals(device):
+    cache = Cache(2, 2, 64, 16, 4, BF, False, 1)
+    q, k, v, gate = new_rows(2, 4, 2, 64, BF, 2)
+    n = i32(3, 4)
+    fn = pa.pi_attn_decode_step_paged
+    c = (cache.k, cache.v, cache.table)
+    for bad in (lambda: fn(n, q[:, :3].contiguous(), k, v, *c, gate[:, :3], 3, 0), lambda: fn(n, q, k[:, :1], v, *c, gate, 3, 0),
+                lambda: fn(n, q, k.float(), v, *c, gate, 3, 0), lambda: fn(n[:1], q, k, v, *c, gate, 3, 0),
+                lambda: fn(n.long(), q, k, v, *c, gate, 3, 0), lambda: fn(n, q, k, v, *c, gate[:, :3], 3, 0),
+                lambda: fn(n, q, k, v, *c, gate, 3, 0, pos=n), lambda: fn(n, q, k, v, *c, gate, 3, 0, freq=frequencies(33).cuda()),
+                lambda: fn(n, q, k, v, *c, gate, 3, 0, freq=frequencies(8).cuda(), sections=(4, 4), pos=n),
+                lambda: fn(n, q, k, v, *c, gate, 1 << 31, 0), lambda: fn(n, q, k, v, *c, gate, 3, 1 << 31),
+                lambda: fn(n, q, k, v, *c, gate, 3, 0, out=torch.empty_like(q[:1])),
+                lambda: fn(n, q, k, v, *c, gate, 3, 0, lse=torch.empty(2, 3, device="cuda")),
+                lambda: fn(n, q.transpose(0, 1).contiguous().transpose(0, 1), k, v, *c, gate, 3, 0)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        fn(n, q.float(), k.float(), v.float(), *c, gate, 3, 0)
+    with pytest.raises(TypeError):
+        fn(n, q, k, v, *c, gate.double(), 3, 0)
+    for kw in (dict(k=-1, pi=0), dict(k=3, pi=-1)):
+        with pytest.raises(pa.PiAttnError):
+            fn(n, q, k, v, *c, gate, kw["k"], kw["pi"])
+    with pytest.raises(pa.PiAttnError):
+        fn(n, q, k, v, *c, gate, 3, 0, len_out=n)

@@ -1,0 +1,221 @@
+"""Rotary positions and their backward against the formula in 64 bits, within bounds derived in
+paged_ref.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_10696_amd as pa
+from tests.cached_ref import f64
+from tests.paged_ref import frequencies, rounded_tol, turned
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+
+
+def data(B, H, N, D, dtype, layout, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(B, N, H, D, generator=g).to(dtype).cuda()
+    return x.transpose(1, 2) if layout == "bnhd" else x.transpose(1, 2).contiguous()
+
+
+def positions(axes, B, N, first, seed):
+    g = torch.Generator().manual_seed(seed)
+    p = torch.arange(N, dtype=torch.int32)[None, None] + first + torch.randint(0, 9, (axes, B, 1), generator=g, dtype=torch.int32)
+    return p.contiguous().cuda()
+
+
+def check(x, got, pos, freq, sections, back=False):
+    y, tol = turned(f64(x), np.asarray(pos.cpu())[:, :, None], freq, sections, back)
+    worst = (np.abs(f64(got) - y) - rounded_tol(y, tol, got.dtype)).max()
+    assert worst <= 0, worst
+
+
+CASES = [
+    # B, H, Hk, N, D, in, out, sections, first position, layout
+    (1, 1, 1, 1, 64, F, F, (32,), 0, "bhnd"),
+    (2, 4, 2, 33, 64, F, F, (32,), 0, "bnhd"),
+    (3, 5, 1, 70, 128, F, BF, (64,), 1000000, "bhnd"),
+    (1, 7, 7, 129, 128, BF, BF, (16, 24, 24), -50, "bnhd"),
+    (2, 3, 2, 17, 64, BF, F, (5, 4, 3), 7, "bhnd"),
+    (5, 2, 1, 9, 128, BF, BF, (1,), 3, "bhnd"),
+    (2, 16, 4, 301, 128, BF, BF, (20, 13), 99, "bnhd"),
+    (1, 9, 9, 40, 64, F, F, (0, 10, 22), 2000000000, "bhnd"),
+    (70, 1, 2, 3, 64, BF, BF, (31,), 12, "bhnd"),
+    (1, 33, 1, 4097, 64, BF, BF, (32,), 0, "bhnd"),
+]
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("case", CASES, ids=[f"{c[0]}x{c[1]}+{c[2]}x{c[3]}x{c[4]}-{len(c[7])}" for c in CASES])
+def test_rotate(device, case, back):
+    B, H, Hk, N, D, dt, to, sections, first, layout = case
+    q, k = data(B, H, N, D, dt, layout, 1), data(B, Hk, N, D, dt, layout, 2)
+    pos, freq = positions(len(sections), B, N, first, 3), frequencies(sum(sections), 1e6).cuda()
+    fn = pa.pi_attn_rotate_backward if back else pa.pi_attn_rotate
+    qo, ko = fn(q, k, pos, freq, sections, dtype=to)
+    assert qo.dtype == ko.dtype == to and qo.is_contiguous() and ko.is_contiguous()
+    check(q, qo, pos, freq, sections, back)
+    check(k, ko, pos, freq, sections, back)
+    # the pairs behind the last one stay, bit by bit
+    P = sum(sections)
+    for x, y in ((q, qo), (k, ko)):
+        for a in (slice(P, D // 2), slice(D // 2 + P, D)):
+            assert torch.equal(x[..., a].to(to), y[..., a])
+
+
+def test_one_axis_and_its_forms(device):
+    """[N], [B, N] and [1, B, N] positions, broadcast and strided ones, none, and a tuple or a list of sections."""
+    q, k = data(2, 3, 50, 64, BF, "bhnd", 1), data(2, 1, 50, 64, BF, "bhnd", 2)
+    freq = frequencies(32).cuda()
+    base = torch.arange(50, dtype=torch.int32, device="cuda")
+    want = pa.pi_attn_rotate(q, k, base[None, None].expand(1, 2, 50).contiguous(), freq, (32,))
+    wide = torch.stack([base, base + 1], 1)
+    for pos, sections in ((None, None), (base, None), (base[None].expand(2, 50), None), (base[None, None].expand(1, 2, 50), (32,)),
+                          (wide[:, 0], [32]), (base.expand(2, 50), (32,))):
+        got = pa.pi_attn_rotate(q, k, pos, freq, sections)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_in_place_and_given_outputs(device):
+    q, k = data(2, 3, 50, 128, BF, "bnhd", 1), data(2, 2, 50, 128, BF, "bhnd", 2)
+    pos, freq = positions(3, 2, 50, 5, 3), frequencies(64).cuda()
+    want = pa.pi_attn_rotate(q, k, pos, freq, (20, 22, 22))
+    q_out = torch.empty(2, 50, 3, 128, dtype=BF, device="cuda").transpose(1, 2)
+    got = pa.pi_attn_rotate(q, k, pos, freq, (20, 22, 22), q_out=q_out)
+    assert got[0] is q_out or got[0].data_ptr() == q_out.data_ptr()
+    assert torch.equal(q_out, want[0]) and torch.equal(got[1], want[1])
+    pa.pi_attn_rotate(q, k, pos, freq, (20, 22, 22), q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_views_of_one_projection(device):
+    """q and k as parts of one tensor, in place: v between and behind them is left as it was."""
+    qkv = data(2, 3 + 2 + 2, 40, 64, BF, "bnhd", 1)
+    before = qkv.clone()
+    q, k = qkv[:, :3], qkv[:, 3:5]
+    pos, freq = positions(1, 2, 40, 5, 3), frequencies(32).cuda()
+    want = pa.pi_attn_rotate(q.clone(), k.clone(), pos, freq)
+    pa.pi_attn_rotate(q, k, pos, freq, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(qkv[:, 5:], before[:, 5:])
+
+
+def test_without_keys(device):
+    q = data(2, 3, 50, 64, F, "bhnd", 1)
+    pos, freq = positions(1, 2, 50, 5, 3), frequencies(32).cuda()
+    got = pa.pi_attn_rotate(q, None, pos, freq)
+    assert got[1] is None
+    check(q, got[0], pos, freq, (32,))
+
+
+@pytest.mark.parametrize("shape", [(0, 3, 5), (2, 3, 0), (2, 0, 5)])
+def test_nothing_to_do(device, shape):
+    B, H, N = shape
+    q = torch.zeros(B, H, N, 64, device="cuda")
+    got = pa.pi_attn_rotate(q, None, None, frequencies(32).cuda())
+    assert got[0].shape == q.shape
+
+
+def test_special_values_stay_with_their_pair(device):
+    """An infinity or NaN in one element reaches the two elements of its pair, or only itself where the pair is not turned."""
+    q = torch.ones(1, 1, 6, 64, device="cuda")
+    q[0, 0, 1, 3], q[0, 0, 2, 40], q[0, 0, 3, 25], q[0, 0, 4, 60] = float("inf"), float("nan"), float("nan"), float("-inf")
+    out, _ = pa.pi_attn_rotate(q, None, None, frequencies(20).cuda())
+    bad = ~torch.isfinite(out[0, 0])
+    want = torch.zeros(6, 64, dtype=torch.bool, device="cuda")
+    for r, cols in ((1, (3, 35)), (2, (8, 40)), (3, (25,)), (4, (60,))):
+        for c in cols:
+            want[r, c] = True
+    assert torch.equal(bad, want)
+    assert out[0, 0, 4, 60] == float("-inf") and torch.isnan(out[0, 0, 3, 25])
+
+
+def test_backward_is_the_gradient(device):
+    """<w, rotate(x)> has the gradient rotate_backward(w): against differences (the map is linear, so any step will do)
+    and against autograd of the formula in 64 bits."""
+    x, w = data(1, 2, 6, 64, F, "bhnd", 1), data(1, 2, 6, 64, F, "bhnd", 2)
+    pos, freq, sections = positions(3, 1, 6, 11, 3), frequencies(30).cuda(), (10, 12, 8)
+    grad, _ = pa.pi_attn_rotate_backward(w, None, pos, freq, sections)
+    leaf = x.cpu().double().requires_grad_()
+    axis = torch.tensor([0] * 10 + [1] * 12 + [2] * 8)
+    angle = pos.cpu().double()[axis].permute(1, 2, 0)[:, None] * freq.cpu().double()
+    a, b = leaf[..., :30], leaf[..., 32:62]
+    c, s = angle.cos(), angle.sin()
+    y = torch.cat([a * c - b * s, leaf[..., 30:32], a * s + b * c, leaf[..., 62:]], -1)
+    y.backward(w.cpu().double())
+    tol = (w.cpu().double().abs().sum(-1, keepdim=True)) * 2.0 ** -20
+    assert ((grad.cpu().double() - leaf.grad).abs() <= tol).all()
+    base = pa.pi_attn_rotate(x, None, pos, freq, sections)[0].double()
+    for i in (0, 5, 31, 33, 61, 63):
+        moved = x.clone()
+        moved[..., i] += 1.0
+        diff = ((pa.pi_attn_rotate(moved, None, pos, freq, sections)[0].double() - base) * w.double()).sum(-1)
+        # four results of the formula, each within 2^-20 of its pair's size
+        size = (x.abs()[..., i] + 2 + x.abs()[..., (i + 32) % 64]).double() * w.double().abs().sum(-1)
+        assert ((diff - grad[..., i].double()).abs() <= 2.0 ** -18 * size).all()
+
+
+def test_backward_undoes_it(device):
+    q, k = data(2, 3, 100, 128, F, "bhnd", 1), data(2, 3, 100, 128, F, "bhnd", 2)
+    pos, freq = positions(3, 2, 100, 100000, 3), frequencies(64).cuda()
+    y = pa.pi_attn_rotate(q, k, pos, freq, (16, 24, 24))
+    z = pa.pi_attn_rotate_backward(*y, pos, freq, (16, 24, 24))
+    for a, b in zip((q, k), z):
+        size = a.abs() + a.abs().roll(64, -1)
+        assert ((a - b).abs() <= 2.0 ** -18 * size).all()
+
+
+def test_attention_depends_on_differences(device):
+    """Scores of turned queries and keys depend on how far apart they are: moving all positions changes the attention by
+    float32 roundings alone."""
+    q, k, v = (data(1, 2, 200, 64, F, "bhnd", i) for i in range(3))
+    gate, freq = torch.zeros(2, device="cuda"), frequencies(32).cuda()
+    outs = []
+    for first in (0, 50000):
+        pos = torch.arange(200, dtype=torch.int32, device="cuda") + first
+        a, b = pa.pi_attn_rotate(q, k, pos, freq)
+        outs.append(pa.pi_attn_forward(a, b, v, gate, 40, 64))
+    # scores of 64 products up to 8 in size, each turned within 2^-19; weights twice that, values up to 5
+    assert (outs[0] - outs[1]).abs().max() <= 64 * 2.0 ** -19 * 8 * 2 / 8 * 5
+
+
+def test_on_a_given_stream(device):
+    q, k = data(2, 3, 500, 64, BF, "bhnd", 1), data(2, 3, 500, 64, BF, "bhnd", 2)
+    pos, freq = positions(1, 2, 500, 5, 3), frequencies(32).cuda()
+    want = pa.pi_attn_rotate(q, k, pos, freq)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    got = pa.pi_attn_rotate(q, k, pos, freq, stream=st)
+    st.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_python_path_alike(device, monkeypatch):
+    q, k = data(2, 3, 50, 64, BF, "bnhd", 1), data(2, 1, 50, 64, BF, "bhnd", 2)
+    pos, freq = positions(2, 2, 50, 5, 3), frequencies(31).cuda()
+    want = pa.pi_attn_rotate(q, k, pos, freq, (20, 11)), pa.pi_attn_rotate_backward(q, k, pos, freq, (20, 11), dtype=F)
+    monkeypatch.setattr(pa, "_native", pa._PythonOnly)
+    got = pa.pi_attn_rotate(q, k, pos, freq, (20, 11)), pa.pi_attn_rotate_backward(q, k, pos, freq, (20, 11), dtype=F)
+    for w, g in zip(want, got):
+        assert torch.equal(w[0], g[0]) and torch.equal(w[1], g[1])
+
+
+def test_refusals(device):
+    q, k = data(2, 3, 50, 64, BF, "bhnd", 1), data(2, 1, 50, 64, BF, "bhnd", 2)
+    freq, pos = frequencies(32).cuda(), positions(1, 2, 50, 0, 1)
+    for bad in (lambda: pa.pi_attn_rotate(q, k[:1], pos, freq), lambda: pa.pi_attn_rotate(q, k[:, :, :49], pos, freq),
+                lambda: pa.pi_attn_rotate(q, k, pos[..., :49], freq), lambda: pa.pi_attn_rotate(q, k, pos, freq, (16, 16)),
+                lambda: pa.pi_attn_rotate(q, k, pos, freq, (31,)), lambda: pa.pi_attn_rotate(q, k, pos, freq, (33, -1)),
+                lambda: pa.pi_attn_rotate(q, k, pos, frequencies(33).cuda()), lambda: pa.pi_attn_rotate(q, k, pos, None),
+                lambda: pa.pi_attn_rotate(q, k, pos, freq.double()), lambda: pa.pi_attn_rotate(q, None, pos, freq, k_out=k),
+                lambda: pa.pi_attn_rotate(q, k, pos, freq, q_out=torch.empty_like(q[:1])),
+                lambda: pa.pi_attn_rotate(q.transpose(2, 3), None, pos, freq)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: pa.pi_attn_rotate(q, k, pos.long(), freq), lambda: pa.pi_attn_rotate(q.half(), None, pos, freq)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(pa.PiAttnError):   # rows of an output that meet
+        pa.pi_attn_rotate(q, None, pos, freq, q_out=torch.empty(2, 1, 50, 64, dtype=BF, device="cuda").expand(2, 3, 50, 64))
+    with pytest.raises(RuntimeError):
+        pa.pi_attn_rotate(q, k, pos.cpu(), freq)
