@@ -17,21 +17,12 @@
 // What bounds it: HBM.
 #include <algorithm>
 
-#include "e4m3.h"
 #include "half_rows.h"
-#include "paged.h"
-#include "pi_common.h"
+#include "paged_step.h"
 
 namespace pi_attn {
 
 namespace {
-
-constexpr float kTau = 8.0f;   // the running maximum is raised in steps above this, log2 units
-
-template <typename ST>
-constexpr bool kQuantised = false;
-template <>
-constexpr bool kQuantised<e4m3> = true;
 
 // What a lane holds of a cached row.
 template <typename ST, int EPL>
@@ -58,20 +49,6 @@ __device__ inline void load_wide(const T *from, float (&f)[EPL]) {
         for (int e = 0; e < N; ++e) f[i * N + e] = x[e];
     }
 }
-
-// The page of a sequence's position, -1 where it has none.
-__device__ inline int page_of(const Pages &g, int64_t s, uint32_t slot) {
-    const int entry = g.table[s * g.max_pages + slot];
-    return entry >= 0 && entry < g.n_pages ? entry : -1;
-}
-
-// Whether sequence s can take a row at t.
-__device__ inline bool has_place(const Pages &g, int64_t s, int t) {
-    return t >= 0 && t < (int64_t)g.page * g.max_pages && page_of(g, s, g.by_page.div(t)) >= 0;
-}
-
-// Ranges that a window of n rows has.
-__device__ inline int ranges_of(int n, int range) { return max(1, (n + range - 1) / range); }
 
 template <typename T, typename ST, int D, int QN, bool PART, int WAVES, int CH>
 __global__ __launch_bounds__(64 * WAVES) void decode_paged_kernel(PagedStepParams p, int q_groups) {
@@ -436,6 +413,11 @@ __global__ __launch_bounds__(256) void join_kernel(PagedStepParams p) {
     }
 }
 
+template <typename T>
+hipError_t launch_join(const PagedStepParams &p, hipStream_t stream) {
+    return launch_kernel(p.D == 64 ? join_kernel<T, 64> : join_kernel<T, 128>, dim3((unsigned)(p.S * p.H)), dim3(256), stream, p);
+}
+
 template <typename T, typename ST, int D, int QN>
 hipError_t launch_q(const PagedStepParams &p, hipStream_t stream) {
     const int G = p.H / p.Hk, q_groups = (G + QN - 1) / QN;
@@ -443,7 +425,7 @@ hipError_t launch_q(const PagedStepParams &p, hipStream_t stream) {
     if (p.parts) {
         const hipError_t e = launch_kernel(decode_paged_kernel<T, ST, D, QN, true, 4, 4>, dim3((unsigned)(groups * p.parts)),
                                            dim3(256), stream, p, q_groups);
-        return e != hipSuccess ? e : launch_kernel(join_kernel<T, D>, dim3((unsigned)(p.S * p.H)), dim3(256), stream, p);
+        return e != hipSuccess ? e : launch_join<T>(p, stream);
     }
     return launch_kernel(decode_paged_kernel<T, ST, D, QN, false, 4, 4>, dim3((unsigned)groups), dim3(256), stream, p, q_groups);
 }
@@ -474,6 +456,11 @@ void plan_decode_paged(PagedStepParams &p, bool bf16) {
 }
 
 hipError_t launch_decode_paged(const PagedStepParams &p, bool bf16, hipStream_t stream) {
+    if ((p.pages.k_exp || bf16) && p.H / p.Hk > 1) {
+        const hipError_t e = launch_decode_paged_tiles(p, bf16, stream);
+        if (e != hipSuccess || !p.parts) return e;
+        return bf16 ? launch_join<__bf16>(p, stream) : launch_join<float>(p, stream);
+    }
     if (p.pages.k_exp) return bf16 ? launch_t<__bf16, e4m3>(p, stream) : launch_t<float, e4m3>(p, stream);
     return bf16 ? launch_t<__bf16, __bf16>(p, stream) : launch_t<float, float>(p, stream);
 }
