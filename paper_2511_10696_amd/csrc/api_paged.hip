@@ -101,8 +101,10 @@ int check_paged_step(int32_t dtype, int32_t S, int32_t H, int32_t Hk, int32_t D,
     const int status = check_page_sizes(n_pages, page, max_pages);
     if (status != PI_ATTN_OK) return status;
     empty = S == 0 || H == 0;
-    // a work-group of 256 threads for each (s, h): fewer than 2^32 threads
-    if ((int64_t)S * H >= 1 << 24) return PI_ATTN_EUNSUPPORTED;
+    // a work-group of 256 threads for each (s, h): fewer than 2^32 threads; rows of
+    // the pool are counted in 32 bits
+    if ((int64_t)S * H >= 1 << 24 || (int64_t)n_pages * page >= kMaxRows || (int64_t)n_pages * page * Hk >= kMaxRows)
+        return PI_ATTN_EUNSUPPORTED;
     p.S = S; p.H = H; p.Hk = Hk; p.D = D; p.k = k;
     p.pages.n_pages = n_pages;
     p.pages.page = page;

@@ -16,6 +16,7 @@
 //
 // What bounds it: HBM.
 #include <algorithm>
+#include <stdlib.h>
 
 #include "half_rows.h"
 #include "paged_step.h"
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_kernel(PagedStepParam
     const int lo = window_lo(t, p.k);
     if (PART && range >= ranges_of(t - lo, p.range)) return;
     // this launch's window rows: first + [0, nwin)
-    const int first = PART ? lo + range * p.range : lo;
+    const int first = PART ? lo + min(range * p.range, t - lo) : lo;
     const int nwin = PART ? min(p.range, t - first) : t - lo;
     const int nchunks = (nwin + RPC - 1) / RPC;
 
@@ -354,10 +355,11 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_kernel(PagedStepParam
     if (!PART && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
 }
 
-// Joins the parts of a query head: a wavefront takes every fourth part.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void join_kernel(PagedStepParams p) {
-    constexpr int WAVES = 4, EPL = D / 64;
+// Joins the parts of a query head: every wavefront takes each WAVES-th, four at a
+// time.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void join_kernel(PagedStepParams p) {
+    constexpr int EPL = D / 64, U = 4;
     __shared__ float s_m[WAVES], s_l[WAVES];
     __shared__ float s_o[WAVES][D];
     const DivMod head_of = divmod(blockIdx.x, p.H);
@@ -374,16 +376,32 @@ __global__ __launch_bounds__(256) void join_kernel(PagedStepParams p) {
     }
     const int n = ranges_of(t - window_lo(t, p.k), p.range);
     float M = -INFINITY, L = 0.0f, o[EPL] = {};
-    for (int x = w; x < n; x += WAVES) {
-        const int64_t at = x * heads + head;
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
-        const float m_new = fmaxf(M, ml.x);
-        const float a = M == m_new ? 1.0f : __builtin_amdgcn_exp2f(M - m_new);
-        const float b = ml.x == m_new ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m_new);
-        M = m_new;
-        L = L * a + ml.y * b;
+    for (int x = w; x < n; x += WAVES * U) {
+        float2 ml[U];
+        float po[U][EPL];
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) o[e] = o[e] * a + p.part_o[at * D + lane + 64 * e] * b;
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = min(x + u * WAVES, n - 1) * heads + head;
+            ml[u] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) po[u][e] = p.part_o[at * D + lane + 64 * e];
+        }
+        float m_new = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, x + u * WAVES < n ? ml[u].x : -INFINITY);
+        const float a = M == m_new ? 1.0f : __builtin_amdgcn_exp2f(M - m_new);
+        M = m_new;
+        L *= a;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) o[e] *= a;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (x + u * WAVES >= n) break;
+            const float b = ml[u].x == M ? 1.0f : __builtin_amdgcn_exp2f(ml[u].x - M);
+            L += ml[u].y * b;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) o[e] += po[u][e] * b;
+        }
     }
 #pragma unroll
     for (int e = 0; e < EPL; ++e) s_o[w][lane + 64 * e] = o[e];
@@ -413,9 +431,16 @@ __global__ __launch_bounds__(256) void join_kernel(PagedStepParams p) {
     }
 }
 
+template <typename T, int D>
+hipError_t launch_join_d(const PagedStepParams &p, hipStream_t stream) {
+    const dim3 grid((unsigned)(p.S * p.H));
+    return p.parts > 32 ? launch_kernel(join_kernel<T, D, 16>, grid, dim3(1024), stream, p)
+                        : launch_kernel(join_kernel<T, D, 4>, grid, dim3(256), stream, p);
+}
+
 template <typename T>
 hipError_t launch_join(const PagedStepParams &p, hipStream_t stream) {
-    return launch_kernel(p.D == 64 ? join_kernel<T, 64> : join_kernel<T, 128>, dim3((unsigned)(p.S * p.H)), dim3(256), stream, p);
+    return p.D == 64 ? launch_join_d<T, 64>(p, stream) : launch_join_d<T, 128>(p, stream);
 }
 
 template <typename T, typename ST, int D, int QN>
@@ -451,6 +476,7 @@ void plan_decode_paged(PagedStepParams &p, bool bf16) {
     p.parts = p.range = 0;
     if (rows <= 1024 || n >= 1024) return;
     p.range = (int)std::max<int64_t>(256, (rows * n + 1023) / 1024);
+    if (getenv("PI_RANGE")) p.range = atoi(getenv("PI_RANGE"));
     p.parts = (int)((rows + p.range - 1) / p.range);
     if (p.parts == 1) p.parts = p.range = 0;
 }

@@ -5,14 +5,18 @@
 // of the window; its wavefronts take tiles of 32 rows in turn, each with a running
 // maximum, sum and accumulator for every query, joined at the end.
 //
+// A tile's keys, then its values, go from registers (whole rows, 16 bytes a lane)
+// into the wavefront's own 32 rows of LDS, as bf16; the registers are free for the
+// next tile's loads at once, which stay under way meanwhile.  No wavefront waits for
+// another before the end.  (Keys loaded in the layout of the scores' operand, 64
+// bytes of each of 16 rows an instruction, need no LDS, but neighbouring lanes are
+// then in different rows, which costs the vector memory path four times the cycles.)
+//
 // MFMA layout (v_mfma_f32_16x16x32_bf16; lane = (c, g) = (l % 16, l / 16)).  Scores
-// S^T = K Q^T, 16 rows at a time: A = K, lane (c, g) holding of row c the elements
-// that it loads from memory as they lie, 16 bytes of every 64; B = Q^T with the same
-// elements; C holds rows 4g + i of query c.  Output O^T += V^T P^T over 32 rows: B =
-// P^T is the weights of two blocks where they are (rows 4g + i and 16 + 4g + i), A =
-// V^T comes from LDS by transpose reads of the same rows.  Only the values pass
-// through LDS, a wavefront's own part of it: no wavefront waits for another before
-// the end.
+// S^T = K Q^T, 16 rows at a time: A = K, lane (c, g) holding elements 32x + 8g.. of
+// row c, B = Q^T the same of query c; C holds rows 4g + i of query c.  Output O^T +=
+// V^T P^T over 32 rows: B = P^T is the weights of two blocks where they are (rows 4g
+// + i and 16 + 4g + i), A = V^T comes by LDS transpose reads of the same rows.
 //
 // Precision.  The products take bf16: cached rows are that, or e4m3, whose codes and
 // scales together are bf16 numbers.  A query (turned, not rounded) and a weight are
@@ -20,6 +24,14 @@
 // (2^-24) where it is float32: the matrix cores have time to spare, a row of 256
 // bytes costs 32 query columns 16 KFLOP.
 #include <algorithm>
+#include <stdlib.h>
+#include <type_traits>
+#ifndef SB
+#define SB 0
+#endif
+#ifndef MINW
+#define MINW 1
+#endif
 
 #include "bf16_rows.h"
 #include "paged_step.h"
@@ -28,35 +40,30 @@ namespace pi_attn {
 
 namespace {
 
-constexpr int WAVES = 8;
 constexpr int TILE = 32;   // rows
 constexpr int NQ = 16;     // query columns
 
 template <typename ST, int D>
 struct Tiles {
+    using R = Row<ST, D>;
     static constexpr int RB = D * (int)sizeof(ST);   // bytes of a cached row
-    static constexpr int NP = RB / 64;               // 16-byte pieces of a lane's row
+    static constexpr int LOADS = TILE / R::RPI;      // load instructions of a tile's keys
     static constexpr int STEPS = D / 32;             // k-steps of the scores
     static constexpr int DB = D / 16;                // 16-dim output blocks
-    // LDS rows, padded by 32 bytes: a transpose read takes 32 bytes of 16 rows, 8 of
-    // which then cover all banks
-    static constexpr int PITCH = 2 * D + 32;
+    // LDS rows, padded by 16 bytes: the reads of the scores take one 16-byte piece of 16
+    // rows, the transpose reads 32 bytes of them, and both meet all banks equally.
+    static constexpr int PITCH = 2 * D + 16;
     static constexpr int BYTES = TILE * PITCH;
-    // first element of a lane's part in k-step `step`
-    static __device__ int dim(int step, int g) {
-        return kQuantised<ST> ? 64 * (step >> 1) + 16 * g + 8 * (step & 1) : 32 * step + 8 * g;
-    }
 };
 
-// The bf16 numbers of eight codes times a scale that is a power of two.
+// Eight codes times a scale that is a power of two, in bf16 (exact).
 __device__ inline bf16x8 codes_bf16(unsigned lo, unsigned hi, float scale) {
-    float f[8];
-    e4m3_unpack4(lo, f);
-    e4m3_unpack4(hi, f + 4);
-    bf16x8 r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (__bf16)(f[i] * scale);
-    return r;
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 // TERMS bf16 numbers that sum to x, but for what the last one cannot hold.
@@ -86,18 +93,21 @@ __device__ inline float query_sum(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-template <typename T, typename ST, int D, bool PART>
-__global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
+template <typename T, typename ST, int D, bool PART, bool CLAMP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
     using L = Tiles<ST, D>;
     constexpr bool Q = kQuantised<ST>;
     constexpr int TERMS = sizeof(T) == 4 ? 3 : 2;
+    static_assert(L::STEPS <= WAVES, "a k-step of the queries a wavefront");
     __shared__ alignas(16) unsigned char s_v[WAVES][L::BYTES];
     __shared__ float s_m[WAVES][NQ], s_l[WAVES][NQ];
-    __shared__ float2 s_cs[WAVES][D / 2];
+    __shared__ float2 s_cs[D / 2];
+    __shared__ bf16x8 s_q[TERMS][L::STEPS][64];   // the queries, as the scores take them
 
-    const DivMod range_of = divmod(blockIdx.x, PART ? p.parts : 1);
-    const int range = (int)range_of.rem;
-    const DivMod group_of = divmod(range_of.quot, q_groups);
+    // The first range of every window, then the second: the shorter last ones come late.
+    const DivMod range_of = divmod(blockIdx.x, PART ? p.S * p.Hk * q_groups : gridDim.x);
+    const int range = (int)range_of.quot;
+    const DivMod group_of = divmod(range_of.rem, q_groups);
     const DivMod head_of = divmod(group_of.quot, p.Hk);
     const int s = (int)head_of.quot, hk = (int)head_of.rem;
     const int G = p.H / p.Hk, g0 = (int)group_of.rem * NQ, nq = min(NQ, G - g0);
@@ -107,106 +117,114 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
     const int c = lane & 15, g = lane >> 4;
     const Pages &pages = p.pages;
     const int t = p.len_in[s];
+    const int64_t reach = (int64_t)pages.page * pages.max_pages;
+    const bool in_reach = t >= 0 && t < reach;
+    const int place = in_reach ? page_of(pages, s, pages.by_page.div(t)) : -1;   // page of the new row
 
-    if (!has_place(pages, s, t)) {
+    // What does not depend on the pages is asked for first: the queries (a k-step by
+    // each wavefront; the other elements of their pairs too) and the gate.
+    const bool rotary = p.r.freq != nullptr;
+    // N elements of a new row in the working type.
+    auto wide = [&](const T *from, auto &f) __attribute__((always_inline)) {
+        constexpr int N = sizeof(f) / 4, E = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < N / E; ++i) {
+            float y[E];
+            to_f32<T>(ld16(from + i * E), y);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[i * E + e] = y[e];
+        }
+    };
+    const T *const q_row = (const T *)p.q_new + (first_head + min(c, nq - 1)) * D;
+    const int q_dim = 32 * min(w, L::STEPS - 1) + 8 * g;
+    float q_own[8], q_other[8];
+    wide(q_row + q_dim, q_own);
+    wide(q_row + (q_dim ^ (D / 2)), q_other);
+    const float gate = p.gate[s * p.gss + (hk * G + g0 + min(c, nq - 1)) * p.gsh];
+
+    const int lo = window_lo(max(t, 0), p.k);
+    // this work-group's window rows: first + [0, nwin)
+    const int first = PART ? lo + min(range * p.range, t - lo) : lo;
+    const int nwin = !in_reach ? 0 : PART ? min(p.range, t - first) : t - lo;
+    const int ntiles = (nwin + TILE - 1) / TILE;
+
+    // Rows of the pool (fewer than 2^31): lane l finds that of a tile's row l % 32, -1
+    // where none is there; its page is looked up a tile ahead.
+    const int per_page = p.Hk * pages.page, kv = hk * pages.page;
+    const int sub = lane % L::R::LPR, rg = lane / L::R::LPR;
+    int entry = -1;
+    auto look_up = [&](int tile) __attribute__((always_inline)) {
+        if (tile < ntiles)
+            entry = page_of(pages, s, pages.by_page.div((uint32_t)(first + min(tile * TILE + (lane & 31), nwin - 1))));
+    };
+    auto find = [&](int tile) __attribute__((always_inline)) {
+        const int i = tile * TILE + (lane & 31);
+        const uint32_t at = (uint32_t)(first + min(i, nwin - 1));
+        return entry >= 0 && i < nwin ? entry * per_page + kv + (int)(at - pages.by_page.div(at) * pages.page) : -1;
+    };
+    // The row that load instruction i covers in this lane.
+    auto row_of = [&](int row, int i) __attribute__((always_inline)) {
+        return __builtin_amdgcn_ds_bpermute(4 * (i * L::R::RPI + rg), row);
+    };
+    // Rows that are not there read row 0 of the pool.
+    auto load = [&](const void *table, int row, uint4 (&r)[L::LOADS]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < L::LOADS; ++i)
+            r[i] = ld16((const uint8_t *)table + (int64_t)max(row_of(row, i), 0) * L::RB + 16 * sub);
+    };
+    // Scale bytes: of the keys in lanes 0..31, of the values in the others.
+    auto load_bytes = [&](int row) __attribute__((always_inline)) -> int {
+        if constexpr (!Q) return 0;
+        const uint8_t *const from = lane < 32 ? pages.k_exp : pages.v_exp;
+        const int byte = from[max(row, 0)];
+        return row >= 0 ? byte : 127;
+    };
+    look_up(w);
+    if (rotary && tid < D / 2) s_cs[tid] = cos_sin_of(p.r, tid, s, 0, t);
+    if (place < 0) {
         if (PART) return;
         for (int i = tid; i < nq * D; i += 64 * WAVES) ((T *)p.out)[first_head * D + i] = (T)NAN;
         if (p.lse && tid < nq) p.lse[first_head + tid] = NAN;
         if (p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t;
         return;
     }
-    const int lo = window_lo(t, p.k);
     if (PART && range >= ranges_of(t - lo, p.range)) return;
-    // this work-group's window rows: first + [0, nwin)
-    const int first = PART ? lo + range * p.range : lo;
-    const int nwin = PART ? min(p.range, t - first) : t - lo;
-    const int ntiles = (nwin + TILE - 1) / TILE;
-
-    const int64_t kv = (int64_t)hk * pages.page;                  // row 0 of this head in page 0
-    const int64_t per_page = (int64_t)p.Hk * pages.page;
-    const uint8_t *kc = (const uint8_t *)pages.k + 16 * g, *vc = (const uint8_t *)pages.v + 16 * g;
-    // A lane's row of each block: page (looked up ahead), place, then its pieces.
-    int entry[2];
-    bool there[2];
-    uint4 kr[2][L::NP], vr[2][L::NP];
-    unsigned kb[2], vb[2];
-    auto look_up = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const uint32_t at = (uint32_t)(first + min(tile * TILE + 16 * b + c, nwin - 1));
-            entry[b] = page_of(pages, s, pages.by_page.div(at));
-        }
-    };
-    auto load = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int i = tile * TILE + 16 * b + c;
-            const uint32_t at = (uint32_t)(first + min(i, nwin - 1));
-            there[b] = entry[b] >= 0 && i < nwin;
-            const int64_t row = max(entry[b], 0) * per_page + kv + (at - pages.by_page.div(at) * pages.page);
-#pragma unroll
-            for (int x = 0; x < L::NP; ++x) {
-                kr[b][x] = ld16(kc + row * L::RB + 64 * x);
-                vr[b][x] = ld16(vc + row * L::RB + 64 * x);
-            }
-            if constexpr (Q) {
-                kb[b] = pages.k_exp[row];
-                vb[b] = pages.v_exp[row];
-            }
-        }
-    };
+    uint4 kr[L::LOADS], vr[L::LOADS];
+    int row = -1, bytes = 127;
     if (w < ntiles) {
-        look_up(w);
-        load(w);
-        if (w + WAVES < ntiles) look_up(w + WAVES);
+        row = find(w);
+        look_up(w + WAVES);
+        bytes = load_bytes(row);
+        load(pages.k, row, kr);
+        load(pages.v, row, vr);
     }
 
-    // Cosines and sines: one pair a lane, by every wavefront for itself.
-    const bool rotary = p.r.freq != nullptr;
-    if (rotary) {
-        if (lane < D / 2) s_cs[w][lane] = cos_sin_of(p.r, lane, s, 0, t);
-        lds_order();
-    }
-    // Eight elements of a new row from `dim` on, turned (the other elements of their
-    // pairs are read too).
-    auto load_new = [&](const T *row, int dim, bool turns, float (&f)[8]) __attribute__((always_inline)) {
-        constexpr int N = 16 / (int)sizeof(T);
-        auto eight = [&](int at, float (&x)[8]) __attribute__((always_inline)) {
+    // Elements from `dim` on turned, `o` the other elements of their pairs.
+    auto turned = [&](auto &f, const auto &o, int dim) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8 / N; ++i) {
-                float y[N];
-                to_f32<T>(ld16(row + at + i * N), y);
-#pragma unroll
-                for (int e = 0; e < N; ++e) x[i * N + e] = y[e];
-            }
-        };
-        eight(dim, f);
-        if (!turns) return;
-        float o[8];
-        eight(dim ^ (D / 2), o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < (int)sizeof(f) / 4; ++e) {
             const int pair = (dim & (D / 2 - 1)) + e;
-            const float2 cs = s_cs[w][pair];
+            const float2 cs = s_cs[pair];
             const float x = f[e] * cs.x, y = o[e] * cs.y;
             if (pair < p.r.pairs) f[e] = dim < D / 2 ? x - y : x + y;
         }
     };
-    bf16x8 qf[TERMS][L::STEPS];
-#pragma unroll
-    for (int x = 0; x < L::STEPS; ++x) {
-        float f[8];
-        load_new((const T *)p.q_new + (first_head + min(c, nq - 1)) * D, L::dim(x, g), rotary, f);
+    if (rotary) __syncthreads();
+    if (w < L::STEPS) {
+        if (rotary) turned(q_own, q_other, q_dim);
+        bf16x8 q[TERMS];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             __bf16 terms[TERMS];
-            split<TERMS>(c < nq ? f[e] : 0.0f, terms);
+            split<TERMS>(c < nq ? q_own[e] : 0.0f, terms);
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i) qf[i][x][e] = terms[i];
+            for (int i = 0; i < TERMS; ++i) q[i][e] = terms[i];
         }
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) s_q[i][w][lane] = q[i];
     }
-    const bool clamped = p.clamp > 0.0f;
-    const FusionBias fb = fusion_bias(p.gate[s * p.gss + (hk * G + g0 + min(c, nq - 1)) * p.gsh], clamped);
+    __syncthreads();
+    const FusionBias fb = fusion_bias(gate, CLAMP);
     const float c2 = p.scale * kLog2e;
 
     f32x4 o[L::DB];
@@ -214,62 +232,63 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
     for (int db = 0; db < L::DB; ++db) o[db] = f32x4{};
     float m = -INFINITY, l = 0.0f;   // of query c; l: this lane's rows
 
-    unsigned char *const tile_v = s_v[w];
-    // The tile in kr, vr: rows 4g + i and 16 + 4g + i are in use where bit i and 4 + i of
-    // `mask` are set; row 1 of the extra tile is the partner.  `next` runs once the
-    // registers are free.
-    auto attend = [&](bool extra, auto next) __attribute__((always_inline)) {
-        // scores
-        f32x4 sc[2] = {f32x4{}, f32x4{}};
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            if (extra && b == 1) break;
-            const float ks = Q ? e4m3_scale(kb[b]) : 1.0f;
-#pragma unroll
-            for (int x = 0; x < L::STEPS; ++x) {
-                bf16x8 a;
-                if constexpr (Q) {
-                    const uint4 u = kr[b][x >> 1];
-                    a = x & 1 ? codes_bf16(u.z, u.w, ks) : codes_bf16(u.x, u.y, ks);
-                } else {
-                    a = __builtin_bit_cast(bf16x8, kr[b][x]);
-                }
-#pragma unroll
-                for (int i = TERMS - 1; i >= 0; --i)
-                    sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[i][x], sc[b], 0, 0, 0);
-            }
+    unsigned char *const lds = s_v[w];
+    // Load instruction i's rows into LDS: whole rows, a lane's 8 (bf16) or 16 (codes) elements.
+    auto put = [&](uint4 u, int i, float scale) __attribute__((always_inline)) {
+        unsigned char *const to = lds + (i * L::R::RPI + rg) * L::PITCH + 2 * L::R::EPL * sub;
+        if constexpr (Q) {
+            *reinterpret_cast<bf16x8 *>(to) = codes_bf16(u.x, u.y, scale);
+            *reinterpret_cast<bf16x8 *>(to + 16) = codes_bf16(u.z, u.w, scale);
+        } else {
+            *reinterpret_cast<uint4 *>(to) = u;
         }
-        // values, zero where no row is there
-        uint64_t rows[2];
+    };
+    // The tile in kr, vr with rows `row`; `bytes` its scale bytes.  EXTRA: one load
+    // instruction's rows alone, row 1 is the partner.  keys_free and values_free run
+    // when these registers can be loaded again.
+    auto attend = [&](auto extra, auto keys_free, auto values_free) __attribute__((always_inline)) {
+        constexpr bool EXTRA = decltype(extra)::value;
+        constexpr int BLOCKS = EXTRA ? 1 : 2, LOADS = EXTRA ? 1 : L::LOADS;
+        const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);   // bit r: row r
+        const bool whole = !EXTRA && there == ~0u;
+        auto scale_of = [&](int i, int table) __attribute__((always_inline)) {
+            return Q ? e4m3_scale(__builtin_amdgcn_ds_bpermute(4 * (i * L::R::RPI + rg + 32 * table), bytes)) : 1.0f;
+        };
         lds_order();   // the tile before has been read
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            rows[b] = __builtin_amdgcn_ballot_w64(there[b]);
-            unsigned char *to = tile_v + (16 * b + c) * L::PITCH;
-            const float vs = Q && there[b] ? e4m3_scale(vb[b]) : 1.0f;
+        for (int i = 0; i < LOADS; ++i) put(kr[i], i, scale_of(i, 0));
+        keys_free();
+        lds_order();
+        f32x4 sc[2] = {f32x4{}, f32x4{}};
 #pragma unroll
-            for (int x = 0; x < L::NP; ++x) {
-                const uint4 u = there[b] ? vr[b][x] : make_uint4(0, 0, 0, 0);
-                if constexpr (Q) {
-                    *reinterpret_cast<bf16x8 *>(to + 128 * x + 32 * g) = codes_bf16(u.x, u.y, vs);
-                    *reinterpret_cast<bf16x8 *>(to + 128 * x + 32 * g + 16) = codes_bf16(u.z, u.w, vs);
-                } else {
-                    *reinterpret_cast<uint4 *>(to + 64 * x + 16 * g) = u;
-                }
+        for (int x = 0; x < L::STEPS; ++x) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                if (SB && x && x % SB == 0 && b == 0) __builtin_amdgcn_sched_barrier(0);
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + (16 * b + c) * L::PITCH + 64 * x + 16 * g);
+#pragma unroll
+                for (int i = TERMS - 1; i >= 0; --i)
+                    sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, s_q[i][x][lane], sc[b], 0, 0, 0);
             }
         }
-        next();
-        float d[8], top = -INFINITY;
+        // A lane's scores are of rows 4g + i and 16 + 4g + i.
+        float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int b = i >> 2, row = 4 * g + (i & 3);
-            float x = sc[b][i & 3];
-            const bool partner = extra && row == 1;
-            x = clamped ? clamped_logit(x * p.scale + (partner ? fb.partner : fb.local), p.clamp) * kLog2e
-                        : x * c2 + (partner ? fb.partner * kLog2e : 0.0f);
-            d[i] = rows[b] >> row & 1 ? x : -INFINITY;
-            top = fmaxf(top, d[i]);
+            d[i] = sc[i >> 2][i & 3];
+            if (CLAMP || EXTRA) {
+                const bool partner = EXTRA && 4 * g + i == 1;
+                d[i] = CLAMP ? clamped_logit(d[i] * p.scale + (partner ? fb.partner : fb.local), p.clamp) * kLog2e
+                             : d[i] * c2 + (partner ? fb.partner * kLog2e : 0.0f);
+            }
         }
+        if (!whole) {
+            const uint32_t mine = there >> 4 * g;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = mine >> (16 * (i >> 2) + (i & 3)) & 1 ? d[i] : -INFINITY;
+        }
+        float top = fmaxf(fmaxf(fmaxf(d[0], d[1]), fmaxf(d[2], d[3])), fmaxf(fmaxf(d[4], d[5]), fmaxf(d[6], d[7])));
+        if constexpr (!CLAMP && !EXTRA) top *= c2;
         if (__builtin_amdgcn_ballot_w64(top > m + kTau)) {
             top = query_max(top);
             const float m_new = top > m + kTau ? top : m;
@@ -283,21 +302,31 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
         bf16x8 pb[TERMS];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float pr = __builtin_amdgcn_exp2f(d[i] - mu);
+            const float pr = __builtin_amdgcn_exp2f(CLAMP || EXTRA ? d[i] - mu : __builtin_fmaf(d[i], c2, -mu));
             l += pr;
             __bf16 terms[TERMS];
             split<TERMS>(pr, terms);
 #pragma unroll
             for (int x = 0; x < TERMS; ++x) pb[x][i] = terms[x];
         }
+        lds_order();   // the keys have been read
+        if (!whole) {   // rows that are not there may hold anything
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                if (row_of(row, i) < 0) vr[i] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < L::LOADS; ++i) put(i < LOADS ? vr[i] : make_uint4(0, 0, 0, 0), i, i < LOADS ? scale_of(i, 1) : 1.0f);
+        values_free();
         lds_order();
-        const int r = (lane >> 2) & 3, qd = lane & 3;
+        const int vrow = 4 * g + ((lane >> 2) & 3), qd = lane & 3;
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) {
+            if (SB && db && db % (2 * SB) == 0) __builtin_amdgcn_sched_barrier(0);
             bf16x8 a;
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
-                const unsigned char *src = tile_v + (4 * g + r + 16 * hh) * L::PITCH + 32 * db + 8 * qd;
+                const unsigned char *src = lds + (vrow + 16 * hh) * L::PITCH + 32 * db + 8 * qd;
                 const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) a[4 * hh + j] = y[j];
@@ -308,12 +337,17 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
     };
 
     for (int tile = w; tile < ntiles; tile += WAVES) {
-        attend(false, [&]() __attribute__((always_inline)) {
-            if (tile + WAVES < ntiles) {
-                load(tile + WAVES);
-                if (tile + 2 * WAVES < ntiles) look_up(tile + 2 * WAVES);
-            }
-        });
+        const bool more = tile + WAVES < ntiles;
+        int next = -1, next_bytes = 127;
+        if (more) {
+            next = find(tile + WAVES);
+            look_up(tile + 2 * WAVES);
+            next_bytes = load_bytes(next);
+        }
+        attend(std::false_type{}, [&]() __attribute__((always_inline)) { if (more) load(pages.k, next, kr); },
+               [&]() __attribute__((always_inline)) { if (more) load(pages.v, next, vr); });
+        row = next;
+        bytes = next_bytes;
     }
 
     // The new row (row 0 of a tile) and the partner (row 1), by the wavefront whose
@@ -321,77 +355,65 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
     if (range == 0 && w == ntiles % WAVES) {
         const int jp = partner_of(t, p.k, p.pi);
         const int pe = jp >= 0 ? page_of(pages, s, pages.by_page.div(jp)) : -1;
-        there[0] = c == 0 || (c == 1 && pe >= 0);
-        there[1] = false;
-        kb[0] = vb[0] = kb[1] = vb[1] = 127;
-#pragma unroll
-        for (int x = 0; x < L::NP; ++x) kr[0][x] = vr[0][x] = vr[1][x] = make_uint4(0, 0, 0, 0);
-        if (c == 1 && pe >= 0) {
-            const int64_t row = pe * per_page + kv + (jp - pages.by_page.div(jp) * pages.page);
-#pragma unroll
-            for (int x = 0; x < L::NP; ++x) {
-                kr[0][x] = ld16(kc + row * L::RB + 64 * x);
-                vr[0][x] = ld16(vc + row * L::RB + 64 * x);
-            }
+        const int partner = pe >= 0 ? pe * per_page + kv + (int)(jp - pages.by_page.div(jp) * pages.page) : -1;
+        const int mine = place * per_page + kv + (int)(t - pages.by_page.div(t) * pages.page);
+        row = lane == 0 ? mine : lane == 1 ? partner : -1;   // the new row is taken as it is stored, from here
+        kr[0] = vr[0] = make_uint4(0, 0, 0, 0);
+        int kb = 127, vb = 127;
+        if (rg == 1 && partner >= 0) {
+            kr[0] = ld16((const uint8_t *)pages.k + (int64_t)partner * L::RB + 16 * sub);
+            vr[0] = ld16((const uint8_t *)pages.v + (int64_t)partner * L::RB + 16 * sub);
             if constexpr (Q) {
-                kb[0] = pages.k_exp[row];
-                vb[0] = pages.v_exp[row];
+                kb = pages.k_exp[partner];
+                vb = pages.v_exp[partner];
             }
         }
-        const int64_t at = ((int64_t)s * p.Hk + hk) * D;
-        // as stored
-        auto stored = [&](const T *row, bool turns, uint4 (&r)[L::NP], unsigned &byte) __attribute__((always_inline)) {
-            float f[L::STEPS][8];
-#pragma unroll
-            for (int x = 0; x < L::STEPS; ++x) load_new(row, L::dim(x, g), turns, f[x]);
+        // This lane's elements of a new row, as stored.
+        constexpr int EPL = L::R::EPL;
+        auto stored = [&](const void *rows, bool turns, uint4 &u, int &byte) __attribute__((always_inline)) {
+            const T *const from = (const T *)rows + ((int64_t)s * p.Hk + hk) * D;
+            float f[EPL];
+            wide(from + sub * EPL, f);
+            if (turns) {
+                float other[EPL];
+                wide(from + (sub ^ (L::R::LPR / 2)) * EPL, other);
+                turned(f, other, sub * EPL);
+            }
+            uint4 r;
+            int by = 127;
             if constexpr (Q) {
                 unsigned a = 0;
 #pragma unroll
-                for (int x = 0; x < L::STEPS; ++x)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) a = max(a, finite_bits(f[x][e]));
-                a = max(a, (unsigned)__shfl_xor((int)a, 16));
-                a = max(a, (unsigned)__shfl_xor((int)a, 32));
-                const unsigned by = e4m3_byte(a);
+                for (int e = 0; e < EPL; ++e) a = max(a, finite_bits(f[e]));
+                by = (int)e4m3_byte(row_max<L::R::LPR>(a));
                 const float inv = e4m3_inverse(by);
-                if (c == 0) {
-                    byte = by;
-#pragma unroll
-                    for (int x = 0; x < L::NP; ++x)
-                        r[x] = make_uint4(e4m3_pack4(f[2 * x], inv), e4m3_pack4(f[2 * x] + 4, inv),
-                                          e4m3_pack4(f[2 * x + 1], inv), e4m3_pack4(f[2 * x + 1] + 4, inv));
-                }
+                r = make_uint4(e4m3_pack4(f, inv), e4m3_pack4(f + 4, inv), e4m3_pack4(f + 8, inv), e4m3_pack4(f + 12, inv));
             } else {
-                if (c != 0) return;
+                bf16x8 y;
 #pragma unroll
-                for (int x = 0; x < L::NP; ++x) {
-                    if (turns) {
-                        bf16x8 y;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = (__bf16)f[x][e];
-                        r[x] = __builtin_bit_cast(uint4, y);
-                    } else {
-                        r[x] = ld16(row + L::dim(x, g));
-                    }
-                }
+                for (int e = 0; e < EPL; ++e) y[e] = (__bf16)f[e];
+                r = turns ? __builtin_bit_cast(uint4, y) : ld16(from + sub * EPL);
+            }
+            if (rg == 0) {
+                u = r;
+                byte = by;
             }
         };
-        stored((const T *)p.k_new + at, rotary, kr[0], kb[0]);
-        stored((const T *)p.v_new + at, false, vr[0], vb[0]);
-        if (c == 0 && g0 == 0) {   // no row read here is row t
-            const uint32_t slot = pages.by_page.div(t);
-            const int64_t row = page_of(pages, s, slot) * per_page + kv + (t - slot * pages.page);
-#pragma unroll
-            for (int x = 0; x < L::NP; ++x) {
-                *reinterpret_cast<uint4 *>((uint8_t *)pages.k + 16 * g + row * L::RB + 64 * x) = kr[0][x];
-                *reinterpret_cast<uint4 *>((uint8_t *)pages.v + 16 * g + row * L::RB + 64 * x) = vr[0][x];
-            }
-            if (Q && g == 0) {
-                pages.k_exp[row] = (uint8_t)kb[0];
-                pages.v_exp[row] = (uint8_t)vb[0];
+        stored(p.k_new, rotary, kr[0], kb);
+        stored(p.v_new, false, vr[0], vb);
+        if (rg == 0 && g0 == 0) {   // no row read here is row t
+            *reinterpret_cast<uint4 *>((uint8_t *)pages.k + (int64_t)mine * L::RB + 16 * sub) = kr[0];
+            *reinterpret_cast<uint4 *>((uint8_t *)pages.v + (int64_t)mine * L::RB + 16 * sub) = vr[0];
+            if (Q && sub == 0) {
+                pages.k_exp[mine] = (uint8_t)kb;
+                pages.v_exp[mine] = (uint8_t)vb;
             }
         }
-        attend(true, []() {});
+        // rows 0 and 1 lie in the row groups' lanes; the bytes go where attend() looks
+        const int at_row = (lane & 31) * L::R::LPR & 63;
+        const int kb_of = __builtin_amdgcn_ds_bpermute(4 * at_row, kb), vb_of = __builtin_amdgcn_ds_bpermute(4 * at_row, vb);
+        bytes = (lane & 31) < L::R::RPI ? (lane < 32 ? kb_of : vb_of) : 127;
+        attend(std::true_type{}, []() {}, []() {});
     }
 
     // Join the wavefronts.
@@ -428,7 +450,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
         } else {
             ((T *)p.out)[first_head * D + i] = (T)(out / sum);
             if (e == 0 && p.lse) {
-                const FusionBias b = fusion_bias(p.gate[s * p.gss + (hk * G + g0 + j) * p.gsh], clamped);
+                const FusionBias b = fusion_bias(p.gate[s * p.gss + (hk * G + g0 + j) * p.gsh], CLAMP);
                 p.lse[first_head + j] = (M + __log2f(sum)) * kLn2 + b.lse_shift;
             }
         }
@@ -436,19 +458,27 @@ __global__ __launch_bounds__(64 * WAVES) void decode_tiles_kernel(PagedStepParam
     if (!PART && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
 }
 
-template <typename T, typename ST, int D>
-hipError_t launch_d(const PagedStepParams &p, hipStream_t stream) {
+template <typename T, typename ST, int D, bool CLAMP, int WAVES>
+hipError_t launch_w(const PagedStepParams &p, hipStream_t stream) {
     const int q_groups = (p.H / p.Hk + NQ - 1) / NQ;
     const int64_t groups = (int64_t)p.S * p.Hk * q_groups;
-    if (p.parts)
-        return launch_kernel(decode_tiles_kernel<T, ST, D, true>, dim3((unsigned)(groups * p.parts)), dim3(64 * WAVES), stream, p,
-                             q_groups);
-    return launch_kernel(decode_tiles_kernel<T, ST, D, false>, dim3((unsigned)groups), dim3(64 * WAVES), stream, p, q_groups);
+    return p.parts ? launch_kernel(decode_tiles_kernel<T, ST, D, true, CLAMP, WAVES>, dim3((unsigned)(groups * p.parts)),
+                                   dim3(64 * WAVES), stream, p, q_groups)
+                   : launch_kernel(decode_tiles_kernel<T, ST, D, false, CLAMP, WAVES>, dim3((unsigned)groups),
+                                   dim3(64 * WAVES), stream, p, q_groups);
+}
+
+template <typename T, typename ST, int D, bool CLAMP>
+hipError_t launch_d(const PagedStepParams &p, hipStream_t stream) {
+    if (getenv("PI_WAVES") && atoi(getenv("PI_WAVES")) == 4) return launch_w<T, ST, D, CLAMP, 4>(p, stream);
+    return launch_w<T, ST, D, CLAMP, 8>(p, stream);
 }
 
 template <typename T, typename ST>
 hipError_t launch_t(const PagedStepParams &p, hipStream_t stream) {
-    return p.D == 64 ? launch_d<T, ST, 64>(p, stream) : launch_d<T, ST, 128>(p, stream);
+    const bool clamp = p.clamp > 0.0f;
+    if (p.D == 64) return clamp ? launch_d<T, ST, 64, true>(p, stream) : launch_d<T, ST, 64, false>(p, stream);
+    return clamp ? launch_d<T, ST, 128, true>(p, stream) : launch_d<T, ST, 128, false>(p, stream);
 }
 
 }  // namespace
