@@ -63,9 +63,10 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_kernel(PagedStepParam
     __shared__ float s_acc[WAVES][QN][D];
     __shared__ float2 s_cs[WAVES][D / 2];
 
-    const DivMod range_of = divmod(blockIdx.x, PART ? p.parts : 1);
-    const int range = (int)range_of.rem;
-    const DivMod group_of = divmod(range_of.quot, q_groups);
+    // The first range of every window, then the second: the shorter last ones come late.
+    const DivMod range_of = divmod(blockIdx.x, PART ? p.S * p.Hk * q_groups : gridDim.x);
+    const int range = (int)range_of.quot;
+    const DivMod group_of = divmod(range_of.rem, q_groups);
     const DivMod head_of = divmod(group_of.quot, p.Hk);
     const int s = (int)head_of.quot, hk = (int)head_of.rem;
     const int G = p.H / p.Hk, g0 = (int)group_of.rem * QN, nq = min(QN, G - g0);
@@ -84,10 +85,10 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_kernel(PagedStepParam
         return;
     }
     const int lo = window_lo(t, p.k);
-    if (PART && range >= ranges_of(t - lo, p.range)) return;
-    // this launch's window rows: first + [0, nwin)
-    const int first = PART ? lo + min(range * p.range, t - lo) : lo;
-    const int nwin = PART ? min(p.range, t - first) : t - lo;
+    const int len = PART ? range_len(p, t - lo) : t - lo;   // of a range
+    if (range > 0 && (int64_t)range * len >= t - lo) return;
+    // this work-group's window rows: first + [0, nwin)
+    const int first = lo + range * len, nwin = min(len, t - first);
     const int nchunks = (nwin + RPC - 1) / RPC;
 
     const int64_t kv = (int64_t)hk * g.page;                  // row 0 of this head in page 0
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(PagedStepParams p) {
         if (p.len_out && h == 0 && tid == 0) p.len_out[s] = t;
         return;
     }
-    const int n = ranges_of(t - window_lo(t, p.k), p.range);
+    const int n = ranges_of(p, t - window_lo(t, p.k));
     float M = -INFINITY, L = 0.0f, o[EPL] = {};
     for (int x = w; x < n; x += WAVES * U) {
         float2 ml[U];
@@ -471,18 +472,19 @@ hipError_t launch_t(const PagedStepParams &p, hipStream_t stream) {
 }  // namespace
 
 void plan_decode_paged(PagedStepParams &p, bool bf16) {
-    const int64_t n = (int64_t)p.S * p.Hk;
-    const int64_t rows = std::min<int64_t>(p.k, (int64_t)p.pages.page * p.pages.max_pages - 1);
+    const int64_t n = (int64_t)p.S * p.Hk, rows = longest_window(p);
     p.parts = p.range = 0;
-    if (rows <= 1024 || n >= 1024) return;
-    p.range = (int)std::max<int64_t>(256, (rows * n + 1023) / 1024);
-    if (getenv("PI_RANGE")) p.range = atoi(getenv("PI_RANGE"));
-    p.parts = (int)((rows + p.range - 1) / p.range);
-    if (p.parts == 1) p.parts = p.range = 0;
+    if (rows <= 1024 || n >= 4096) return;
+    int64_t r = std::clamp<int64_t>((rows * n / 768 + 127) & ~(int64_t)127, 256, 1024);
+    if (getenv("PI_RANGE")) r = atoi(getenv("PI_RANGE"));
+    const int64_t parts = std::min<int64_t>((rows + r - 1) / r, std::max<int64_t>(1, 4096 / n));
+    if (parts < 2) return;
+    p.range = (int)r;
+    p.parts = (int)parts;
 }
 
 hipError_t launch_decode_paged(const PagedStepParams &p, bool bf16, hipStream_t stream) {
-    if ((p.pages.k_exp || bf16) && p.H / p.Hk > 1) {
+    if ((p.pages.k_exp || bf16) && (p.H / p.Hk > 1 || getenv("PI_TILES"))) {
         const hipError_t e = launch_decode_paged_tiles(p, bf16, stream);
         if (e != hipSuccess || !p.parts) return e;
         return bf16 ? launch_join<__bf16>(p, stream) : launch_join<float>(p, stream);

@@ -26,13 +26,6 @@
 #include <algorithm>
 #include <stdlib.h>
 #include <type_traits>
-#ifndef SB
-#define SB 0
-#endif
-#ifndef MINW
-#define MINW 1
-#endif
-
 #include "bf16_rows.h"
 #include "paged_step.h"
 
@@ -40,6 +33,7 @@ namespace pi_attn {
 
 namespace {
 
+constexpr int WAVES = 4;
 constexpr int TILE = 32;   // rows
 constexpr int NQ = 16;     // query columns
 
@@ -93,8 +87,9 @@ __device__ inline float query_sum(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-template <typename T, typename ST, int D, bool PART, bool CLAMP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
+// ONCE: the window's rows are not kept in the caches.
+template <typename T, typename ST, int D, bool CLAMP, bool ONCE>
+__global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
     using L = Tiles<ST, D>;
     constexpr bool Q = kQuantised<ST>;
     constexpr int TERMS = sizeof(T) == 4 ? 3 : 2;
@@ -104,8 +99,9 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
     __shared__ float2 s_cs[D / 2];
     __shared__ bf16x8 s_q[TERMS][L::STEPS][64];   // the queries, as the scores take them
 
+    const bool part = p.parts != 0;
     // The first range of every window, then the second: the shorter last ones come late.
-    const DivMod range_of = divmod(blockIdx.x, PART ? p.S * p.Hk * q_groups : gridDim.x);
+    const DivMod range_of = divmod(blockIdx.x, part ? p.S * p.Hk * q_groups : gridDim.x);
     const int range = (int)range_of.quot;
     const DivMod group_of = divmod(range_of.rem, q_groups);
     const DivMod head_of = divmod(group_of.quot, p.Hk);
@@ -119,6 +115,9 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
     const int t = p.len_in[s];
     const int64_t reach = (int64_t)pages.page * pages.max_pages;
     const bool in_reach = t >= 0 && t < reach;
+    const int lo = window_lo(max(t, 0), p.k);
+    const int len = part ? range_len(p, t - lo) : t - lo;   // of a range
+    if (in_reach && range > 0 && (int64_t)range * len >= t - lo) return;
     const int place = in_reach ? page_of(pages, s, pages.by_page.div(t)) : -1;   // page of the new row
 
     // What does not depend on the pages is asked for first: the queries (a k-step by
@@ -142,10 +141,9 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
     wide(q_row + (q_dim ^ (D / 2)), q_other);
     const float gate = p.gate[s * p.gss + (hk * G + g0 + min(c, nq - 1)) * p.gsh];
 
-    const int lo = window_lo(max(t, 0), p.k);
     // this work-group's window rows: first + [0, nwin)
-    const int first = PART ? lo + min(range * p.range, t - lo) : lo;
-    const int nwin = !in_reach ? 0 : PART ? min(p.range, t - first) : t - lo;
+    const int first = lo + range * len;
+    const int nwin = in_reach ? min(len, t - first) : 0;
     const int ntiles = (nwin + TILE - 1) / TILE;
 
     // Rows of the pool (fewer than 2^31): lane l finds that of a tile's row l % 32, -1
@@ -169,8 +167,10 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
     // Rows that are not there read row 0 of the pool.
     auto load = [&](const void *table, int row, uint4 (&r)[L::LOADS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < L::LOADS; ++i)
-            r[i] = ld16((const uint8_t *)table + (int64_t)max(row_of(row, i), 0) * L::RB + 16 * sub);
+        for (int i = 0; i < L::LOADS; ++i) {
+            const uint8_t *const from = (const uint8_t *)table + (int64_t)max(row_of(row, i), 0) * L::RB + 16 * sub;
+            r[i] = ONCE ? ld16_once(from) : ld16(from);
+        }
     };
     // Scale bytes: of the keys in lanes 0..31, of the values in the others.
     auto load_bytes = [&](int row) __attribute__((always_inline)) -> int {
@@ -182,13 +182,12 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
     look_up(w);
     if (rotary && tid < D / 2) s_cs[tid] = cos_sin_of(p.r, tid, s, 0, t);
     if (place < 0) {
-        if (PART) return;
+        if (part) return;
         for (int i = tid; i < nq * D; i += 64 * WAVES) ((T *)p.out)[first_head * D + i] = (T)NAN;
         if (p.lse && tid < nq) p.lse[first_head + tid] = NAN;
         if (p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t;
         return;
     }
-    if (PART && range >= ranges_of(t - lo, p.range)) return;
     uint4 kr[L::LOADS], vr[L::LOADS];
     int row = -1, bytes = 127;
     if (w < ntiles) {
@@ -264,7 +263,6 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
         for (int x = 0; x < L::STEPS; ++x) {
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
-                if (SB && x && x % SB == 0 && b == 0) __builtin_amdgcn_sched_barrier(0);
                 const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + (16 * b + c) * L::PITCH + 64 * x + 16 * g);
 #pragma unroll
                 for (int i = TERMS - 1; i >= 0; --i)
@@ -322,7 +320,6 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
         const int vrow = 4 * g + ((lane >> 2) & 3), qd = lane & 3;
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) {
-            if (SB && db && db % (2 * SB) == 0) __builtin_amdgcn_sched_barrier(0);
             bf16x8 a;
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
@@ -443,7 +440,7 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
             sum += s_l[x][j] * f;
             out += s_o[(x * nq + j) * D + e] * f;
         }
-        if (PART) {
+        if (part) {
             const int64_t at = (int64_t)range * p.S * p.H + first_head + j;
             p.part_o[at * D + e] = out;
             if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * at) = make_float2(M, sum);
@@ -455,23 +452,20 @@ __global__ __launch_bounds__(64 * WAVES, MINW) void decode_tiles_kernel(PagedSte
             }
         }
     }
-    if (!PART && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
+    if (!part && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
 }
 
-template <typename T, typename ST, int D, bool CLAMP, int WAVES>
-hipError_t launch_w(const PagedStepParams &p, hipStream_t stream) {
-    const int q_groups = (p.H / p.Hk + NQ - 1) / NQ;
-    const int64_t groups = (int64_t)p.S * p.Hk * q_groups;
-    return p.parts ? launch_kernel(decode_tiles_kernel<T, ST, D, true, CLAMP, WAVES>, dim3((unsigned)(groups * p.parts)),
-                                   dim3(64 * WAVES), stream, p, q_groups)
-                   : launch_kernel(decode_tiles_kernel<T, ST, D, false, CLAMP, WAVES>, dim3((unsigned)groups),
-                                   dim3(64 * WAVES), stream, p, q_groups);
-}
+// ONCE, by the bytes of the windows' rows, which are read once where one work-group has
+// all of a key head's queries.
+constexpr int64_t kKeepBytes = 12 << 20;
 
 template <typename T, typename ST, int D, bool CLAMP>
 hipError_t launch_d(const PagedStepParams &p, hipStream_t stream) {
-    if (getenv("PI_WAVES") && atoi(getenv("PI_WAVES")) == 4) return launch_w<T, ST, D, CLAMP, 4>(p, stream);
-    return launch_w<T, ST, D, CLAMP, 8>(p, stream);
+    const int q_groups = (p.H / p.Hk + NQ - 1) / NQ;
+    const int64_t groups = (int64_t)p.S * p.Hk * q_groups, rows = longest_window(p);
+    const bool once = q_groups == 1 && 2 * groups * rows * D * (int64_t)sizeof(ST) > kKeepBytes && !getenv("PI_KEEP");
+    return launch_kernel(once ? decode_tiles_kernel<T, ST, D, CLAMP, true> : decode_tiles_kernel<T, ST, D, CLAMP, false>,
+                         dim3((unsigned)(groups * std::max(p.parts, 1))), dim3(64 * WAVES), stream, p, q_groups);
 }
 
 template <typename T, typename ST>

@@ -1,6 +1,8 @@
 // paged_step.h -- what the kernels of the decode step over paged caches share.
 #pragma once
 
+#include <algorithm>
+
 #include "decode_rows.h"
 #include "e4m3.h"
 #include "paged.h"
@@ -28,8 +30,21 @@ __device__ inline bool has_place(const Pages &g, int64_t s, int t) {
     return t >= 0 && t < (int64_t)g.page * g.max_pages && page_of(g, s, g.by_page.div(t)) >= 0;
 }
 
-// Ranges that a window of n rows has.
-__device__ inline int ranges_of(int n, int range) { return max(1, (n + range - 1) / range); }
+// Rows of the longest window that the cache can hold, the new row apart.
+inline int64_t longest_window(const PagedStepParams &p) {
+    return std::min<int64_t>(p.k, (int64_t)p.pages.page * p.pages.max_pages - 1);
+}
+
+// Rows of a range, and ranges, of a window of n rows in a split step: p.range, more
+// where that would be more than p.parts ranges; whole steps of 128 rows.
+__device__ inline int range_len(const PagedStepParams &p, int n) {
+    const int even = (int)((((int64_t)n + p.parts - 1) / p.parts + 127) & ~(int64_t)127);
+    return max(p.range, even);
+}
+__device__ inline int ranges_of(const PagedStepParams &p, int n) {
+    const int len = range_len(p, n);
+    return max(1, (int)(((int64_t)n + len - 1) / len));
+}
 
 // A step of which pages in bf16 or e4m3 are multiplied on the matrix cores.
 hipError_t launch_decode_paged_tiles(const PagedStepParams &p, bool bf16, hipStream_t stream);
