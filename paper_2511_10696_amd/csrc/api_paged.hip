@@ -109,7 +109,7 @@ int check_paged_step(int32_t dtype, int32_t S, int32_t H, int32_t Hk, int32_t D,
     p.pages.n_pages = n_pages;
     p.pages.page = page;
     p.pages.max_pages = max_pages;
-    if (!empty) plan_decode_paged(p, dtype == PI_ATTN_BF16);
+    if (!empty) plan_decode_paged(p);
     return PI_ATTN_OK;
 }
 

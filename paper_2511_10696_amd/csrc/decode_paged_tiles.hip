@@ -24,8 +24,6 @@
 // (2^-24) where it is float32: the matrix cores have time to spare, a row of 256
 // bytes costs 32 query columns 16 KFLOP.
 #include <algorithm>
-#include <stdlib.h>
-#include <type_traits>
 #include "bf16_rows.h"
 #include "paged_step.h"
 
@@ -33,8 +31,7 @@ namespace pi_attn {
 
 namespace {
 
-constexpr int WAVES = 4;
-constexpr int TILE = 32;   // rows
+constexpr int TILE = 32;   // rows, two blocks of 16
 constexpr int NQ = 16;     // query columns
 
 template <typename ST, int D>
@@ -88,15 +85,18 @@ __device__ inline float query_sum(float x) {
 }
 
 // ONCE: the window's rows are not kept in the caches.
-template <typename T, typename ST, int D, bool CLAMP, bool ONCE>
-__global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
+template <typename T, typename ST, int D, bool CLAMP, bool ONCE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_kernel(PagedStepParams p, int q_groups) {
     using L = Tiles<ST, D>;
     constexpr bool Q = kQuantised<ST>;
     constexpr int TERMS = sizeof(T) == 4 ? 3 : 2;
     static_assert(L::STEPS <= WAVES, "a k-step of the queries a wavefront");
-    __shared__ alignas(16) unsigned char s_v[WAVES][L::BYTES];
+    // a tile's rows for each wavefront; its accumulators at the end
+    __shared__ alignas(16) unsigned char s_v[WAVES * L::BYTES];
     __shared__ float s_m[WAVES][NQ], s_l[WAVES][NQ];
     __shared__ float2 s_cs[D / 2];
+    __shared__ uint4 s_new[2][L::R::LPR];         // the new row, as it is stored
+    __shared__ unsigned s_new_bytes[2];           // and its scale bytes
     __shared__ bf16x8 s_q[TERMS][L::STEPS][64];   // the queries, as the scores take them
 
     const bool part = p.parts != 0;
@@ -134,6 +134,16 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
             for (int e = 0; e < E; ++e) f[i * E + e] = y[e];
         }
     };
+    // Wavefront 0 makes the new row: a lane the piece that it would load of any row.
+    constexpr int EPL = L::R::EPL;
+    const int sub = lane % L::R::LPR, rg = lane / L::R::LPR;
+    float k_own[EPL], k_other[EPL], v_own[EPL];
+    if (w == 0) {
+        const int64_t at = ((int64_t)s * p.Hk + hk) * D;
+        wide((const T *)p.k_new + at + sub * EPL, k_own);
+        wide((const T *)p.k_new + at + (sub ^ (L::R::LPR / 2)) * EPL, k_other);
+        wide((const T *)p.v_new + at + sub * EPL, v_own);
+    }
     const T *const q_row = (const T *)p.q_new + (first_head + min(c, nq - 1)) * D;
     const int q_dim = 32 * min(w, L::STEPS - 1) + 8 * g;
     float q_own[8], q_other[8];
@@ -141,41 +151,49 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
     wide(q_row + (q_dim ^ (D / 2)), q_other);
     const float gate = p.gate[s * p.gss + (hk * G + g0 + min(c, nq - 1)) * p.gsh];
 
-    // this work-group's window rows: first + [0, nwin)
+    // This work-group's rows: the window's, first + [0, nwin), and behind those of the
+    // last range the new one and the partner.
     const int first = lo + range * len;
     const int nwin = in_reach ? min(len, t - first) : 0;
-    const int ntiles = (nwin + TILE - 1) / TILE;
+    const bool last = first + nwin == t;
+    const int jp = partner_of(t, p.k, p.pi);
+    const int nrows = nwin + (last ? jp >= 0 ? 2 : 1 : 0);
+    const int ntiles = (nrows + TILE - 1) / TILE;
 
-    // Rows of the pool (fewer than 2^31): lane l finds that of a tile's row l % 32, -1
+    // Rows of the pool (fewer than 2^31): lane l finds that of a tile's row l % TILE, -1
     // where none is there; its page is looked up a tile ahead.
     const int per_page = p.Hk * pages.page, kv = hk * pages.page;
-    const int sub = lane % L::R::LPR, rg = lane / L::R::LPR;
+    const int32_t *const table = pages.table + (int64_t)s * pages.max_pages;
     int entry = -1;
+    auto position = [&](int tile) __attribute__((always_inline)) {
+        const int i = min(tile * TILE + lane % TILE, nrows - 1);
+        return (uint32_t)(i < nwin ? first + i : i == nwin ? t : jp);
+    };
     auto look_up = [&](int tile) __attribute__((always_inline)) {
-        if (tile < ntiles)
-            entry = page_of(pages, s, pages.by_page.div((uint32_t)(first + min(tile * TILE + (lane & 31), nwin - 1))));
+        if (tile < ntiles) entry = table[pages.by_page.div(position(tile))];   // not looked at here: no wait
     };
     auto find = [&](int tile) __attribute__((always_inline)) {
-        const int i = tile * TILE + (lane & 31);
-        const uint32_t at = (uint32_t)(first + min(i, nwin - 1));
-        return entry >= 0 && i < nwin ? entry * per_page + kv + (int)(at - pages.by_page.div(at) * pages.page) : -1;
+        const uint32_t at = position(tile);
+        return page_named(pages, entry) >= 0 && tile * TILE + lane % TILE < nrows
+                   ? entry * per_page + kv + (int)(at - pages.by_page.div(at) * pages.page)
+                   : -1;
     };
     // The row that load instruction i covers in this lane.
     auto row_of = [&](int row, int i) __attribute__((always_inline)) {
         return __builtin_amdgcn_ds_bpermute(4 * (i * L::R::RPI + rg), row);
     };
     // Rows that are not there read row 0 of the pool.
-    auto load = [&](const void *table, int row, uint4 (&r)[L::LOADS]) __attribute__((always_inline)) {
+    auto load = [&](const void *rows, int row, uint4 (&r)[L::LOADS]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < L::LOADS; ++i) {
-            const uint8_t *const from = (const uint8_t *)table + (int64_t)max(row_of(row, i), 0) * L::RB + 16 * sub;
+            const uint8_t *const from = (const uint8_t *)rows + (int64_t)max(row_of(row, i), 0) * L::RB + 16 * sub;
             r[i] = ONCE ? ld16_once(from) : ld16(from);
         }
     };
-    // Scale bytes: of the keys in lanes 0..31, of the values in the others.
+    // Scale bytes: of the keys in the first TILE lanes, of the values in the next.
     auto load_bytes = [&](int row) __attribute__((always_inline)) -> int {
         if constexpr (!Q) return 0;
-        const uint8_t *const from = lane < 32 ? pages.k_exp : pages.v_exp;
+        const uint8_t *const from = lane < TILE ? pages.k_exp : pages.v_exp;
         const int byte = from[max(row, 0)];
         return row >= 0 ? byte : 127;
     };
@@ -209,6 +227,46 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
         }
     };
     if (rotary) __syncthreads();
+    if (w == 0 && last) {
+        if (rotary) turned(k_own, k_other, sub * EPL);
+        // as stored: in the pages' type
+        auto stored = [&](const float (&f)[EPL], uint4 &u) __attribute__((always_inline)) {
+            if constexpr (Q) {
+                unsigned a = 0;
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) a = max(a, finite_bits(f[e]));
+                const unsigned byte = e4m3_byte(row_max<L::R::LPR>(a));
+                const float inv = e4m3_inverse(byte);
+                u = make_uint4(e4m3_pack4(f, inv), e4m3_pack4(f + 4, inv), e4m3_pack4(f + 8, inv), e4m3_pack4(f + 12, inv));
+                return byte;
+            } else {
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) y[e] = (__bf16)f[e];
+                u = __builtin_bit_cast(uint4, y);
+                return 127u;
+            }
+        };
+        uint4 kx, vx;
+        const unsigned kb = stored(k_own, kx), vb = stored(v_own, vx);
+        if (rg == 0) {
+            s_new[0][sub] = kx;
+            s_new[1][sub] = vx;
+            if (sub == 0) {
+                s_new_bytes[0] = kb;
+                s_new_bytes[1] = vb;
+            }
+            if (g0 == 0) {   // of row t nothing is used that is read here
+                const int64_t mine = place * per_page + kv + (int)(t - pages.by_page.div(t) * pages.page);
+                *reinterpret_cast<uint4 *>((uint8_t *)pages.k + mine * L::RB + 16 * sub) = kx;
+                *reinterpret_cast<uint4 *>((uint8_t *)pages.v + mine * L::RB + 16 * sub) = vx;
+                if (Q && sub == 0) {
+                    pages.k_exp[mine] = (uint8_t)kb;
+                    pages.v_exp[mine] = (uint8_t)vb;
+                }
+            }
+        }
+    }
     if (w < L::STEPS) {
         if (rotary) turned(q_own, q_other, q_dim);
         bf16x8 q[TERMS];
@@ -231,10 +289,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
     for (int db = 0; db < L::DB; ++db) o[db] = f32x4{};
     float m = -INFINITY, l = 0.0f;   // of query c; l: this lane's rows
 
-    unsigned char *const lds = s_v[w];
-    // Load instruction i's rows into LDS: whole rows, a lane's 8 (bf16) or 16 (codes) elements.
-    auto put = [&](uint4 u, int i, float scale) __attribute__((always_inline)) {
-        unsigned char *const to = lds + (i * L::R::RPI + rg) * L::PITCH + 2 * L::R::EPL * sub;
+    unsigned char *const lds = s_v + w * L::BYTES;
+    // A lane's 8 (bf16) or 16 (codes) elements of row r of the tile into LDS.
+    auto put = [&](uint4 u, int r, float scale) __attribute__((always_inline)) {
+        unsigned char *const to = lds + r * L::PITCH + 2 * L::R::EPL * sub;
         if constexpr (Q) {
             *reinterpret_cast<bf16x8 *>(to) = codes_bf16(u.x, u.y, scale);
             *reinterpret_cast<bf16x8 *>(to + 16) = codes_bf16(u.z, u.w, scale);
@@ -242,27 +300,32 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
             *reinterpret_cast<uint4 *>(to) = u;
         }
     };
-    // The tile in kr, vr with rows `row`; `bytes` its scale bytes.  EXTRA: one load
-    // instruction's rows alone, row 1 is the partner.  keys_free and values_free run
-    // when these registers can be loaded again.
-    auto attend = [&](auto extra, auto keys_free, auto values_free) __attribute__((always_inline)) {
-        constexpr bool EXTRA = decltype(extra)::value;
-        constexpr int BLOCKS = EXTRA ? 1 : 2, LOADS = EXTRA ? 1 : L::LOADS;
+    for (int tile = w; tile < ntiles; tile += WAVES) {
+        const bool more = tile + WAVES < ntiles;
+        int next = -1, next_bytes = 127;
+        if (more) {
+            next = find(tile + WAVES);
+            look_up(tile + 2 * WAVES);
+            next_bytes = load_bytes(next);
+        }
         const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);   // bit r: row r
-        const bool whole = !EXTRA && there == ~0u;
+        const bool whole = there == ~0u;
+        const int new_r = nwin - tile * TILE;   // the new row's, where last
+        const bool special = last && new_r < TILE && new_r >= -1;   // it or the partner is in the tile
         auto scale_of = [&](int i, int table) __attribute__((always_inline)) {
-            return Q ? e4m3_scale(__builtin_amdgcn_ds_bpermute(4 * (i * L::R::RPI + rg + 32 * table), bytes)) : 1.0f;
+            return Q ? e4m3_scale(__builtin_amdgcn_ds_bpermute(4 * (i * L::R::RPI + rg + TILE * table), bytes)) : 1.0f;
         };
         lds_order();   // the tile before has been read
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) put(kr[i], i, scale_of(i, 0));
-        keys_free();
+        for (int i = 0; i < L::LOADS; ++i) put(kr[i], i * L::R::RPI + rg, scale_of(i, 0));
+        if (special && new_r >= 0 && rg == 0) put(s_new[0][sub], new_r, e4m3_scale(s_new_bytes[0]));
+        if (more) load(pages.k, next, kr);
         lds_order();
         f32x4 sc[2] = {f32x4{}, f32x4{}};
 #pragma unroll
         for (int x = 0; x < L::STEPS; ++x) {
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
+            for (int b = 0; b < 2; ++b) {
                 const bf16x8 a = *reinterpret_cast<const bf16x8 *>(lds + (16 * b + c) * L::PITCH + 64 * x + 16 * g);
 #pragma unroll
                 for (int i = TERMS - 1; i >= 0; --i)
@@ -270,12 +333,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
             }
         }
         // A lane's scores are of rows 4g + i and 16 + 4g + i.
-        float d[8];
+        float d[8], unit = CLAMP ? 1.0f : c2;   // of d, in log2 units
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            d[i] = sc[i >> 2][i & 3];
-            if (CLAMP || EXTRA) {
-                const bool partner = EXTRA && 4 * g + i == 1;
+        for (int i = 0; i < 8; ++i) d[i] = sc[i >> 2][i & 3];
+        if (CLAMP || special) {
+            unit = 1.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool partner = special && 16 * (i >> 2) + 4 * g + (i & 3) == new_r + 1;
                 d[i] = CLAMP ? clamped_logit(d[i] * p.scale + (partner ? fb.partner : fb.local), p.clamp) * kLog2e
                              : d[i] * c2 + (partner ? fb.partner * kLog2e : 0.0f);
             }
@@ -285,8 +350,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = mine >> (16 * (i >> 2) + (i & 3)) & 1 ? d[i] : -INFINITY;
         }
-        float top = fmaxf(fmaxf(fmaxf(d[0], d[1]), fmaxf(d[2], d[3])), fmaxf(fmaxf(d[4], d[5]), fmaxf(d[6], d[7])));
-        if constexpr (!CLAMP && !EXTRA) top *= c2;
+        float top = d[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, d[i]);
+        top *= unit;
         if (__builtin_amdgcn_ballot_w64(top > m + kTau)) {
             top = query_max(top);
             const float m_new = top > m + kTau ? top : m;
@@ -300,7 +367,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
         bf16x8 pb[TERMS];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float pr = __builtin_amdgcn_exp2f(CLAMP || EXTRA ? d[i] - mu : __builtin_fmaf(d[i], c2, -mu));
+            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(d[i], unit, -mu));
             l += pr;
             __bf16 terms[TERMS];
             split<TERMS>(pr, terms);
@@ -308,14 +375,16 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
             for (int x = 0; x < TERMS; ++x) pb[x][i] = terms[x];
         }
         lds_order();   // the keys have been read
-        if (!whole) {   // rows that are not there may hold anything
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                if (row_of(row, i) < 0) vr[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < L::LOADS; ++i) put(vr[i], i * L::R::RPI + rg, scale_of(i, 1));
+        if (!whole && row < 0) {   // rows that are not there may hold anything
+            constexpr int LANES = 64 / TILE;   // of a row
+            unsigned char *const to = lds + lane % TILE * L::PITCH + lane / TILE * (2 * D / LANES);
+#pragma unroll
+            for (int i = 0; i < 2 * D / LANES; i += 16) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
         }
-#pragma unroll
-        for (int i = 0; i < L::LOADS; ++i) put(i < LOADS ? vr[i] : make_uint4(0, 0, 0, 0), i, i < LOADS ? scale_of(i, 1) : 1.0f);
-        values_free();
+        if (special && new_r >= 0 && rg == 0) put(s_new[1][sub], new_r, e4m3_scale(s_new_bytes[1]));
+        if (more) load(pages.v, next, vr);
         lds_order();
         const int vrow = 4 * g + ((lane >> 2) & 3), qd = lane & 3;
 #pragma unroll
@@ -331,86 +400,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
 #pragma unroll
             for (int x = TERMS - 1; x >= 0; --x) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[x], o[db], 0, 0, 0);
         }
-    };
-
-    for (int tile = w; tile < ntiles; tile += WAVES) {
-        const bool more = tile + WAVES < ntiles;
-        int next = -1, next_bytes = 127;
-        if (more) {
-            next = find(tile + WAVES);
-            look_up(tile + 2 * WAVES);
-            next_bytes = load_bytes(next);
-        }
-        attend(std::false_type{}, [&]() __attribute__((always_inline)) { if (more) load(pages.k, next, kr); },
-               [&]() __attribute__((always_inline)) { if (more) load(pages.v, next, vr); });
         row = next;
         bytes = next_bytes;
-    }
-
-    // The new row (row 0 of a tile) and the partner (row 1), by the wavefront whose
-    // turn comes after the last tile.
-    if (range == 0 && w == ntiles % WAVES) {
-        const int jp = partner_of(t, p.k, p.pi);
-        const int pe = jp >= 0 ? page_of(pages, s, pages.by_page.div(jp)) : -1;
-        const int partner = pe >= 0 ? pe * per_page + kv + (int)(jp - pages.by_page.div(jp) * pages.page) : -1;
-        const int mine = place * per_page + kv + (int)(t - pages.by_page.div(t) * pages.page);
-        row = lane == 0 ? mine : lane == 1 ? partner : -1;   // the new row is taken as it is stored, from here
-        kr[0] = vr[0] = make_uint4(0, 0, 0, 0);
-        int kb = 127, vb = 127;
-        if (rg == 1 && partner >= 0) {
-            kr[0] = ld16((const uint8_t *)pages.k + (int64_t)partner * L::RB + 16 * sub);
-            vr[0] = ld16((const uint8_t *)pages.v + (int64_t)partner * L::RB + 16 * sub);
-            if constexpr (Q) {
-                kb = pages.k_exp[partner];
-                vb = pages.v_exp[partner];
-            }
-        }
-        // This lane's elements of a new row, as stored.
-        constexpr int EPL = L::R::EPL;
-        auto stored = [&](const void *rows, bool turns, uint4 &u, int &byte) __attribute__((always_inline)) {
-            const T *const from = (const T *)rows + ((int64_t)s * p.Hk + hk) * D;
-            float f[EPL];
-            wide(from + sub * EPL, f);
-            if (turns) {
-                float other[EPL];
-                wide(from + (sub ^ (L::R::LPR / 2)) * EPL, other);
-                turned(f, other, sub * EPL);
-            }
-            uint4 r;
-            int by = 127;
-            if constexpr (Q) {
-                unsigned a = 0;
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) a = max(a, finite_bits(f[e]));
-                by = (int)e4m3_byte(row_max<L::R::LPR>(a));
-                const float inv = e4m3_inverse(by);
-                r = make_uint4(e4m3_pack4(f, inv), e4m3_pack4(f + 4, inv), e4m3_pack4(f + 8, inv), e4m3_pack4(f + 12, inv));
-            } else {
-                bf16x8 y;
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) y[e] = (__bf16)f[e];
-                r = turns ? __builtin_bit_cast(uint4, y) : ld16(from + sub * EPL);
-            }
-            if (rg == 0) {
-                u = r;
-                byte = by;
-            }
-        };
-        stored(p.k_new, rotary, kr[0], kb);
-        stored(p.v_new, false, vr[0], vb);
-        if (rg == 0 && g0 == 0) {   // no row read here is row t
-            *reinterpret_cast<uint4 *>((uint8_t *)pages.k + (int64_t)mine * L::RB + 16 * sub) = kr[0];
-            *reinterpret_cast<uint4 *>((uint8_t *)pages.v + (int64_t)mine * L::RB + 16 * sub) = vr[0];
-            if (Q && sub == 0) {
-                pages.k_exp[mine] = (uint8_t)kb;
-                pages.v_exp[mine] = (uint8_t)vb;
-            }
-        }
-        // rows 0 and 1 lie in the row groups' lanes; the bytes go where attend() looks
-        const int at_row = (lane & 31) * L::R::LPR & 63;
-        const int kb_of = __builtin_amdgcn_ds_bpermute(4 * at_row, kb), vb_of = __builtin_amdgcn_ds_bpermute(4 * at_row, vb);
-        bytes = (lane & 31) < L::R::RPI ? (lane < 32 ? kb_of : vb_of) : 127;
-        attend(std::true_type{}, []() {}, []() {});
     }
 
     // Join the wavefronts.
@@ -420,7 +411,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
         s_l[w][c] = l;
     }
     __syncthreads();   // the tiles are done with
-    float *const s_o = reinterpret_cast<float *>(s_v[0]);   // [WAVES][nq][D]
+    float *const s_o = reinterpret_cast<float *>(s_v);   // [WAVES][nq][D]
     static_assert(NQ * D * 4 <= L::BYTES, "a wavefront's accumulators fit its tile");
     if (c < nq) {
 #pragma unroll
@@ -455,17 +446,22 @@ __global__ __launch_bounds__(64 * WAVES, 3) void decode_tiles_kernel(PagedStepPa
     if (!part && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
 }
 
-// ONCE, by the bytes of the windows' rows, which are read once where one work-group has
-// all of a key head's queries.
-constexpr int64_t kKeepBytes = 12 << 20;
+// Eight wavefronts where the work-groups have a CU each, four otherwise, which lets
+// three of them share one (registers and LDS).
+template <typename T, typename ST, int D, bool CLAMP, bool ONCE>
+hipError_t launch_w(const PagedStepParams &p, int64_t groups, int q_groups, hipStream_t stream) {
+    if (p.parts == 0 && groups <= 256)
+        return launch_kernel(decode_tiles_kernel<T, ST, D, CLAMP, ONCE, 8>, dim3((unsigned)groups), dim3(512), stream, p, q_groups);
+    return launch_kernel(decode_tiles_kernel<T, ST, D, CLAMP, ONCE, 4>, dim3((unsigned)(groups * std::max(p.parts, 1))),
+                         dim3(256), stream, p, q_groups);
+}
 
 template <typename T, typename ST, int D, bool CLAMP>
 hipError_t launch_d(const PagedStepParams &p, hipStream_t stream) {
     const int q_groups = (p.H / p.Hk + NQ - 1) / NQ;
-    const int64_t groups = (int64_t)p.S * p.Hk * q_groups, rows = longest_window(p);
-    const bool once = q_groups == 1 && 2 * groups * rows * D * (int64_t)sizeof(ST) > kKeepBytes && !getenv("PI_KEEP");
-    return launch_kernel(once ? decode_tiles_kernel<T, ST, D, CLAMP, true> : decode_tiles_kernel<T, ST, D, CLAMP, false>,
-                         dim3((unsigned)(groups * std::max(p.parts, 1))), dim3(64 * WAVES), stream, p, q_groups);
+    const int64_t groups = (int64_t)p.S * p.Hk * q_groups;
+    return read_once(p, q_groups, sizeof(ST)) ? launch_w<T, ST, D, CLAMP, true>(p, groups, q_groups, stream)
+                                              : launch_w<T, ST, D, CLAMP, false>(p, groups, q_groups, stream);
 }
 
 template <typename T, typename ST>

@@ -59,8 +59,9 @@ struct PagedStepParams {
     float scale, clamp;
     void *out;                      // [S][H][D]
     float *lse;                     // [S][H] or nullptr
-    // Ranges of `range` window rows that leave parts (parts = 0: not split): for
-    // part x at[x][s * H + h] the weighted values [D], then (max, sum) in log2 units.
+    // Parts from ranges of the windows, at least `range` rows each and at most `parts`
+    // of a window (0: not split): for part x at[x][s * H + h] the weighted values [D],
+    // then (max, sum) in log2 units.
     float *part_o, *part_ml;
     int range, parts;
 };
@@ -69,7 +70,7 @@ hipError_t launch_rotate(const RotateParams &p, bool bf16_in, bool bf16_out, hip
 hipError_t launch_paged_rows(const PagedRowsParams &p, bool store, bool bf16, hipStream_t stream);
 
 // The sizes of the parts, by the problem's sizes alone; then the step.
-void plan_decode_paged(PagedStepParams &p, bool bf16);
+void plan_decode_paged(PagedStepParams &p);
 hipError_t launch_decode_paged(const PagedStepParams &p, bool bf16, hipStream_t stream);
 
 }  // namespace pi_attn

@@ -35,6 +35,13 @@ inline int64_t longest_window(const PagedStepParams &p) {
     return std::min<int64_t>(p.k, (int64_t)p.pages.page * p.pages.max_pages - 1);
 }
 
+// Whether a step's window rows are not worth keeping in the caches: they are read once
+// (one work-group has all of a key head's queries), and would push out what is there.
+inline bool read_once(const PagedStepParams &p, int q_groups, int element_bytes) {
+    constexpr int64_t kKeepBytes = 12 << 20;
+    return q_groups == 1 && 2 * (int64_t)p.S * p.Hk * longest_window(p) * p.D * element_bytes > kKeepBytes;
+}
+
 // Rows of a range, and ranges, of a window of n rows in a split step: p.range, more
 // where that would be more than p.parts ranges; whole steps of 128 rows.
 __device__ inline int range_len(const PagedStepParams &p, int n) {
@@ -46,7 +53,9 @@ __device__ inline int ranges_of(const PagedStepParams &p, int n) {
     return max(1, (int)(((int64_t)n + len - 1) / len));
 }
 
-// A step of which pages in bf16 or e4m3 are multiplied on the matrix cores.
+// The step but for the join of its parts: pages in bf16 or e4m3, on the matrix cores; in
+// float32.
 hipError_t launch_decode_paged_tiles(const PagedStepParams &p, bool bf16, hipStream_t stream);
+hipError_t launch_decode_paged_f32(const PagedStepParams &p, hipStream_t stream);
 
 }  // namespace pi_attn
