@@ -18,7 +18,18 @@ constexpr int CH = 4;
 
 __device__ inline void load4(const float *from, float (&f)[4]) { to_f32<float>(ld16(from), f); }
 
-template <int D, int QN, bool ONCE, int WAVES>
+// Sum over the LPR lanes of a row, left in each of them.
+template <int LPR>
+__device__ inline float row_total(float x) {
+    x = row_sum<16>(x);
+    if constexpr (LPR == 32) {   // rows of 16 lanes 0 and 1, 2 and 3
+        const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+    return x;
+}
+
+template <int D, int QN, bool CLAMP, bool ONCE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepParams p, int q_groups) {
     using R = Row<float, D>;
     constexpr int LPR = R::LPR, RPI = R::RPI;
@@ -144,10 +155,9 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
         for (int j = 0; j < QN; ++j) turned((const float *)p.q_new + (first_head + min(j, nq - 1)) * D, q[j]);
     }
     float bias[QN], shift[QN];   // the partner's (and, clamped, the window's) prior
-    const bool clamped = p.clamp > 0.0f;
 #pragma unroll
     for (int j = 0; j < QN; ++j) {
-        const FusionBias fb = fusion_bias(gate[j], clamped);
+        const FusionBias fb = fusion_bias(gate[j], CLAMP);
         bias[j] = fb.partner;
         shift[j] = fb.local;
     }
@@ -170,9 +180,9 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
             float x = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) x += q[j][e] * kf[e];
-            x = row_sum<LPR>(x);
-            d[j] = clamped ? clamped_logit(x * p.scale + (partner ? bias[j] : shift[j]), p.clamp) * kLog2e
-                           : x * c2 + (partner ? bias[j] * kLog2e : 0.0f);
+            x = row_total<LPR>(x);
+            d[j] = CLAMP ? clamped_logit(x * p.scale + (partner ? bias[j] : shift[j]), p.clamp) * kLog2e
+                         : x * c2 + (partner ? bias[j] * kLog2e : 0.0f);
         }
     };
 
@@ -297,7 +307,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
         } else {
             ((float *)p.out)[first_head * D + i] = o / L;
             if (e == 0 && p.lse) {
-                const FusionBias fb = fusion_bias(p.gate[s * p.gss + (hk * G + g0 + j) * p.gsh], clamped);
+                const FusionBias fb = fusion_bias(p.gate[s * p.gss + (hk * G + g0 + j) * p.gsh], CLAMP);
                 p.lse[first_head + j] = (M + __log2f(L)) * kLn2 + fb.lse_shift;
             }
         }
@@ -305,34 +315,36 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
     if (!part && p.len_out && hk == 0 && g0 == 0 && tid == 0) p.len_out[s] = t + 1;
 }
 
-template <int D, int QN, bool ONCE>
+template <int D, int QN, bool CLAMP, bool ONCE>
 hipError_t launch_w(const PagedStepParams &p, int64_t groups, int q_groups, hipStream_t stream) {
     if (p.parts == 0 && groups <= 256)
-        return launch_kernel(decode_paged_f32_kernel<D, QN, ONCE, 8>, dim3((unsigned)groups), dim3(512), stream, p, q_groups);
-    return launch_kernel(decode_paged_f32_kernel<D, QN, ONCE, 4>, dim3((unsigned)(groups * std::max(p.parts, 1))), dim3(256), stream,
+        return launch_kernel(decode_paged_f32_kernel<D, QN, CLAMP, ONCE, 8>, dim3((unsigned)groups), dim3(512), stream, p, q_groups);
+    return launch_kernel(decode_paged_f32_kernel<D, QN, CLAMP, ONCE, 4>, dim3((unsigned)(groups * std::max(p.parts, 1))), dim3(256), stream,
                          p, q_groups);
 }
 
-template <int D, int QN>
+template <int D, int QN, bool CLAMP>
 hipError_t launch_q(const PagedStepParams &p, hipStream_t stream) {
     const int q_groups = (p.H / p.Hk + QN - 1) / QN;
     const int64_t groups = (int64_t)p.S * p.Hk * q_groups;
-    return read_once(p, q_groups, 4) ? launch_w<D, QN, true>(p, groups, q_groups, stream)
-                                     : launch_w<D, QN, false>(p, groups, q_groups, stream);
+    return read_once(p, q_groups, 4) ? launch_w<D, QN, CLAMP, true>(p, groups, q_groups, stream)
+                                     : launch_w<D, QN, CLAMP, false>(p, groups, q_groups, stream);
 }
 
-template <int D>
+template <int D, bool CLAMP>
 hipError_t launch_d(const PagedStepParams &p, hipStream_t stream) {
     const int G = p.H / p.Hk;
-    if (G == 1) return launch_q<D, 1>(p, stream);
-    if (G == 2) return launch_q<D, 2>(p, stream);
-    return G <= 4 ? launch_q<D, 4>(p, stream) : launch_q<D, 8>(p, stream);
+    if (G == 1) return launch_q<D, 1, CLAMP>(p, stream);
+    if (G == 2) return launch_q<D, 2, CLAMP>(p, stream);
+    return G <= 4 ? launch_q<D, 4, CLAMP>(p, stream) : launch_q<D, 8, CLAMP>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_decode_paged_f32(const PagedStepParams &p, hipStream_t stream) {
-    return p.D == 64 ? launch_d<64>(p, stream) : launch_d<128>(p, stream);
+    const bool clamp = p.clamp > 0.0f;
+    if (p.D == 64) return clamp ? launch_d<64, true>(p, stream) : launch_d<64, false>(p, stream);
+    return clamp ? launch_d<128, true>(p, stream) : launch_d<128, false>(p, stream);
 }
 
 }  // namespace pi_attn
