@@ -7,6 +7,22 @@
 
 namespace pi_attn {
 
+// The wavefronts of a launch over tiles of rows and groups of heads: the groups of a
+// tile next to each other, or the tiles of a group.
+struct WaveOrder {
+    bool heads_first;
+    uint32_t tiles, groups;
+    Divisor by_inner;
+    WaveOrder() = default;
+    WaveOrder(bool hf, uint32_t t, uint32_t g) : heads_first(hf), tiles(t), groups(g), by_inner(hf ? g : t) {}
+    // Tile and group of wavefront `wave`; tile is past the last one for those without work.
+    __device__ void place(uint32_t wave, uint32_t &tile, uint32_t &group) const {
+        const uint32_t outer = by_inner.div(wave), inner = wave - outer * (heads_first ? groups : tiles);
+        tile = heads_first || outer >= groups ? (heads_first ? outer : tiles) : inner;
+        group = heads_first ? inner : outer;
+    }
+};
+
 // Rows of q [B][H][N][D] and k [B][Hk][N][D] turned, forward or back.
 struct RotateParams {
     int B, H, Hk, N, D;
@@ -18,8 +34,7 @@ struct RotateParams {
     bool back;                      // the transpose: by the angle's negative
     uint32_t rows;                  // B * N, at least 1
     Divisor by_n;
-    int per, splits;                // heads of a wavefront, and wavefronts for all of them; set by the launch
-    Divisor by_splits;
+    WaveOrder order;                // set by the launch
 };
 
 // A paged cache: position j of sequence s is row j mod page of page
@@ -42,8 +57,7 @@ struct PagedRowsParams {
     Rotary r;                       // of the keys stored
     uint32_t rows;                  // S * n, at least 1
     Divisor by_n;
-    int per, splits;                // as of RotateParams
-    Divisor by_splits;
+    WaveOrder order;                // set by the launch
 };
 
 // A decode step over a paged cache: H query heads, H / Hk to a key head.

@@ -3,11 +3,15 @@
 // 128.  A store turns the keys by their positions on the way (rotary.h), in fp32,
 // with one rounding to what the page holds.
 //
-// A wavefront takes a few rows of one sequence (as many as one load instruction
-// covers), looks their pages up and forms their cosines and sines once, and walks
-// over the heads.
+// A wavefront takes a few rows (as many as one load instruction covers) and two heads,
+// looks the rows' pages up and forms their cosines and sines once.
 //
-// What bounds it: HBM, rows read and written once.
+// What bounds it: HBM, rows read and written once.  Wavefronts that are next to each
+// other take neighbours in memory: the heads of a row where these lie together
+// ([S][n][H][D], 8 prompts of 3000 to 6000 rows of 16 heads, turned, bf16, D = 128: 101
+// us, 590 MB at 5.8 TB/s, and 114 the other way), the rows of a head otherwise ([S][H]
+// [n][D], 4 of 16000 rows of 8 heads into e4m3: 71 us, 394 MB, and 78).  All heads a
+// wavefront, walked two at a time: 121 and 75.  A plain copy reaches 4.9 TB/s.
 #include <algorithm>
 
 #include "e4m3.h"
@@ -20,7 +24,7 @@ namespace pi_attn {
 namespace {
 
 constexpr int WAVES = 4;
-constexpr int U = 2;   // heads whose loads are in flight together, keys and values
+constexpr int U = 2;   // heads of a wavefront, their keys' and values' loads in flight together
 
 // What a lane does for its row, all heads alike.
 struct Place {
@@ -47,20 +51,31 @@ __device__ inline bool place(const PagedRowsParams &p, uint32_t tile, int rg, Pl
     return true;
 }
 
-template <typename T, bool QUANT, int D, bool ONCE>
+// LD, SD: what is loaded, or stored, is not kept in the caches.
+template <typename T, bool QUANT, int D, bool LD, bool SD>
 __global__ __launch_bounds__(64 * WAVES) void paged_store_kernel(PagedRowsParams p) {
     using R = HalfRow<T, D>;
     constexpr int EPL = R::EPL;
     const int lane = __lane_id(), sub = lane % R::LPR, rg = lane / R::LPR;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + (threadIdx.x >> 6));
-    const uint32_t tile = p.by_splits.div(wave);
+    uint32_t tile, group;
+    p.order.place(wave, tile, group);
     Place a;
-    if (!place<R::RPI>(p, tile, rg, a)) return;
+    if (tile >= p.order.tiles || !place<R::RPI>(p, tile, rg, a)) return;
     if (!a.there) return;   // a row's lanes alike
-    const int h0 = (int)(wave - tile * p.splits) * p.per, h1 = min(h0 + p.per, p.Hk);
+    const int h0 = (int)group * U;
     const int64_t from = a.s * p.sb + a.i * p.sn + sub * EPL;
     const T *k = (const T *)p.k + from, *v = (const T *)p.v + from;
 
+    Piece<T, EPL> kl[U], kh[U], vl[U], vh[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t x = min(h0 + u, p.Hk - 1) * p.sh;
+        kl[u] = load_piece<T, EPL, LD>(k + x);
+        kh[u] = load_piece<T, EPL, LD>(k + x + D / 2);
+        vl[u] = load_piece<T, EPL, LD>(v + x);
+        vh[u] = load_piece<T, EPL, LD>(v + x + D / 2);
+    }
     float2 cs[EPL];
     bool turned[EPL];
     if (p.r.freq) {
@@ -98,45 +113,35 @@ __global__ __launch_bounds__(64 * WAVES) void paged_store_kernel(PagedRowsParams
                 ch.w[i] = e4m3_pack4(y + 4 * i, inv);
             }
             uint8_t *to = (uint8_t *)pages + row * D + sub * EPL;
-            store_piece<uint8_t, EPL, ONCE>(cl, to);
-            store_piece<uint8_t, EPL, ONCE>(ch, to + D / 2);
+            store_piece<uint8_t, EPL, SD>(cl, to);
+            store_piece<uint8_t, EPL, SD>(ch, to + D / 2);
             if (sub == 0) exps[row] = (uint8_t)byte;
         } else {
             T *to = (T *)pages + row * D + sub * EPL;
-            store_piece<T, EPL, ONCE>(turns ? narrowed<T, EPL>(x) : lo, to);
-            store_piece<T, EPL, ONCE>(turns ? narrowed<T, EPL>(y) : hi, to + D / 2);
+            store_piece<T, EPL, SD>(turns ? narrowed<T, EPL>(x) : lo, to);
+            store_piece<T, EPL, SD>(turns ? narrowed<T, EPL>(y) : hi, to + D / 2);
         }
     };
-    for (int h = h0; h < h1; h += U) {
-        Piece<T, EPL> kl[U], kh[U], vl[U], vh[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t x = min(h + u, h1 - 1) * p.sh;
-            kl[u] = load_piece<T, EPL, ONCE>(k + x);
-            kh[u] = load_piece<T, EPL, ONCE>(k + x + D / 2);
-            vl[u] = load_piece<T, EPL, ONCE>(v + x);
-            vh[u] = load_piece<T, EPL, ONCE>(v + x + D / 2);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (h + u >= h1) break;
-            put(kl[u], kh[u], p.r.freq != nullptr, h + u, g.k, g.k_exp);
-            put(vl[u], vh[u], false, h + u, g.v, g.v_exp);
-        }
+    for (int u = 0; u < U; ++u) {
+        if (h0 + u >= p.Hk) break;
+        put(kl[u], kh[u], p.r.freq != nullptr, h0 + u, g.k, g.k_exp);
+        put(vl[u], vh[u], false, h0 + u, g.v, g.v_exp);
     }
 }
 
-template <typename T, bool QUANT, int D, bool ONCE>
+template <typename T, bool QUANT, int D, bool LD, bool SD>
 __global__ __launch_bounds__(64 * WAVES) void paged_load_kernel(PagedRowsParams p) {
     using R = HalfRow<T, D>;
     constexpr int EPL = R::EPL;
     using ST = typename std::conditional<QUANT, uint8_t, T>::type;   // what the pages hold
     const int lane = __lane_id(), sub = lane % R::LPR, rg = lane / R::LPR;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + (threadIdx.x >> 6));
-    const uint32_t tile = p.by_splits.div(wave);
+    uint32_t tile, group;
+    p.order.place(wave, tile, group);
     Place a;
-    if (!place<R::RPI>(p, tile, rg, a)) return;
-    const int h0 = (int)(wave - tile * p.splits) * p.per, h1 = min(h0 + p.per, p.Hk);
+    if (tile >= p.order.tiles || !place<R::RPI>(p, tile, rg, a)) return;
+    const int h0 = (int)group * U;
     const int64_t to = a.s * p.sb + a.i * p.sn + sub * EPL;
     T *k = (T *)p.k + to, *v = (T *)p.v + to;
     const Pages &g = p.pages;
@@ -149,55 +154,62 @@ __global__ __launch_bounds__(64 * WAVES) void paged_load_kernel(PagedRowsParams 
             for (int i = 0; i < EPL / 4; ++i) e4m3_unpack4(x.w[i], f + 4 * i);
 #pragma unroll
             for (int e = 0; e < EPL; ++e) f[e] *= scale;
-            store_piece<T, EPL, ONCE>(narrowed<T, EPL>(f), y);
+            store_piece<T, EPL, SD>(narrowed<T, EPL>(f), y);
         } else {
-            store_piece<T, EPL, ONCE>(x, y);
+            store_piece<T, EPL, SD>(x, y);
         }
     };
-    for (int h = h0; h < h1; h += U) {
-        Piece<ST, EPL> x[U][4];
-        unsigned kb[U], vb[U];
+    Piece<ST, EPL> x[U][4];
+    unsigned kb[U], vb[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            kb[u] = vb[u] = 127;
+    for (int u = 0; u < U; ++u) {
+        kb[u] = vb[u] = 127;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[u][j] = Piece<ST, EPL>{};   // absent rows: zeros, in codes too
-            if (a.there) {
-                const int64_t row = a.first + (int64_t)min(h + u, h1 - 1) * g.page;
-                x[u][0] = load_piece<ST, EPL, false>(kp + row * D);
-                x[u][1] = load_piece<ST, EPL, false>(kp + row * D + D / 2);
-                x[u][2] = load_piece<ST, EPL, false>(vp + row * D);
-                x[u][3] = load_piece<ST, EPL, false>(vp + row * D + D / 2);
-                if constexpr (QUANT) {
-                    kb[u] = g.k_exp[row];
-                    vb[u] = g.v_exp[row];
-                }
+        for (int j = 0; j < 4; ++j) x[u][j] = Piece<ST, EPL>{};   // absent rows: zeros, in codes too
+        if (a.there) {
+            const int64_t row = a.first + (int64_t)min(h0 + u, p.Hk - 1) * g.page;
+            x[u][0] = load_piece<ST, EPL, LD>(kp + row * D);
+            x[u][1] = load_piece<ST, EPL, LD>(kp + row * D + D / 2);
+            x[u][2] = load_piece<ST, EPL, LD>(vp + row * D);
+            x[u][3] = load_piece<ST, EPL, LD>(vp + row * D + D / 2);
+            if constexpr (QUANT) {
+                kb[u] = g.k_exp[row];
+                vb[u] = g.v_exp[row];
             }
         }
+    }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (h + u >= h1) break;
-            const int64_t y = (h + u) * p.sh;
-            out(x[u][0], kb[u], k + y);
-            out(x[u][1], kb[u], k + y + D / 2);
-            out(x[u][2], vb[u], v + y);
-            out(x[u][3], vb[u], v + y + D / 2);
-        }
+    for (int u = 0; u < U; ++u) {
+        if (h0 + u >= p.Hk) break;
+        const int64_t y = (h0 + u) * p.sh;
+        out(x[u][0], kb[u], k + y);
+        out(x[u][1], kb[u], k + y + D / 2);
+        out(x[u][2], vb[u], v + y);
+        out(x[u][3], vb[u], v + y + D / 2);
     }
 }
+
+// Rows are not kept in the caches from 128 MB on, read and written: 66 MB stored 13.9 us
+// kept and 15.2 not, loaded 11.8 and 13.1; 229 MB 49.2 and 44.2, 47.8 and 41.9.  Loads of
+// halves below 128 bytes share lines, and are kept: e4m3 to bf16, 361 MB, 65.4 us and 70.8.
+constexpr int64_t kKeepBytes = 128 << 20;
 
 template <typename T, bool QUANT, int D>
 hipError_t launch_d(PagedRowsParams p, bool store, hipStream_t stream) {
     using R = HalfRow<T, D>;
-    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI;
-    p.splits = (int)std::clamp<int64_t>(8192 / tiles, 1, (p.Hk + U - 1) / U);
-    p.per = ((p.Hk + p.splits - 1) / p.splits + U - 1) / U * U;
-    p.splits = (p.Hk + p.per - 1) / p.per;
-    p.by_splits = Divisor(p.splits);
-    const int64_t groups = (tiles * p.splits + WAVES - 1) / WAVES;
-    if (groups >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
-    return launch_kernel(store ? paged_store_kernel<T, QUANT, D, false> : paged_load_kernel<T, QUANT, D, false>,
-                         dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
+    constexpr int NARROW = QUANT ? 1 : (int)sizeof(T);   // bytes of an element in the pages
+    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = (p.Hk + U - 1) / U;
+    const int64_t blocks = (tiles * groups + WAVES - 1) / WAVES;
+    if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
+    p.order = WaveOrder(p.sh < p.sn, (uint32_t)tiles, (uint32_t)groups);
+    const bool once = 2 * (int64_t)p.rows * p.Hk * D * (int64_t)(sizeof(T) + NARROW) > kKeepBytes;
+    constexpr bool kStoreLd = D / 2 * sizeof(T) >= 128, kLoadLd = D / 2 * NARROW >= 128;
+    const dim3 grid((unsigned)blocks), block(64 * WAVES);
+    if (store)
+        return launch_kernel(once ? paged_store_kernel<T, QUANT, D, kStoreLd, true> : paged_store_kernel<T, QUANT, D, false, false>,
+                             grid, block, stream, p);
+    return launch_kernel(once ? paged_load_kernel<T, QUANT, D, kLoadLd, true> : paged_load_kernel<T, QUANT, D, false, false>, grid,
+                         block, stream, p);
 }
 
 template <typename T>

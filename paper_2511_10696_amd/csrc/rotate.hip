@@ -3,12 +3,17 @@
 // arithmetic, one rounding at the end.
 //
 // A wavefront takes a few positions (as many as one load instruction covers, a
-// lane holding both halves of its pairs) and walks over heads with the cosines
-// and sines that it forms once; q's and k's heads are one list.  A lane reads all
-// that it writes over before it writes, so that a result may take its input's
-// place.
+// lane holding both halves of its pairs) and four heads, with the cosines and sines
+// that it forms once; q's and k's heads are one list.  A lane reads all that it writes
+// over before it writes, so that a result may take its input's place.
 //
-// What bounds it: HBM, rows read and written once.
+// What bounds it: HBM, rows read and written once.  Wavefronts that are next to each
+// other take neighbours in memory: the heads of a position where these lie together
+// ([B][N][H][D], 8192 positions of 4 x 40 heads, bf16, D = 128: 110 us, 671 MB at 6.1
+// TB/s, and 123 the other way), the positions of a head otherwise ([B][H][N][D], 4 x
+// 32 heads: 89 us and 109).  More heads a wavefront, walked one group after the other,
+// save cosines and lose memory streams: one sequence of 32768, float32 to bf16, 333 us
+// with all 64 heads, 291 with four.  A plain copy reaches 4.9 TB/s.
 #include <algorithm>
 
 #include "half_rows.h"
@@ -20,7 +25,7 @@ namespace pi_attn {
 namespace {
 
 constexpr int WAVES = 4;
-constexpr int U = 4;   // heads whose loads are in flight together
+constexpr int U = 4;   // heads of a wavefront, their loads in flight together
 
 template <typename TI, typename TO, int D, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES) void rotate_kernel(RotateParams p) {
@@ -28,11 +33,12 @@ __global__ __launch_bounds__(64 * WAVES) void rotate_kernel(RotateParams p) {
     constexpr int EPL = R::EPL;
     const int lane = __lane_id(), sub = lane % R::LPR, rg = lane / R::LPR;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + (threadIdx.x >> 6));
-    const uint32_t tile = p.by_splits.div(wave);
+    uint32_t tile, group;
+    p.order.place(wave, tile, group);
     const uint32_t r = tile * R::RPI + rg;
-    if (r >= p.rows) return;
+    if (tile >= p.order.tiles || r >= p.rows) return;
     const uint32_t b = p.by_n.div(r), n = r - b * p.N;
-    const int h0 = (int)(wave - tile * p.splits) * p.per, h1 = min(h0 + p.per, p.H + p.Hk);
+    const int h0 = (int)group * U, heads = p.H + p.Hk;
 
     const TI *q = (const TI *)p.q + b * p.qsb + n * p.qsn + sub * EPL;
     const TI *k = (const TI *)p.k + b * p.ksb + n * p.ksn + sub * EPL;
@@ -47,43 +53,48 @@ __global__ __launch_bounds__(64 * WAVES) void rotate_kernel(RotateParams p) {
         if (p.back) cs[e].y = -cs[e].y;
         turned[e] = i < p.r.pairs;
     }
-    for (int h = h0; h < h1; h += U) {
-        Piece<TI, EPL> lo[U], hi[U];
+    Piece<TI, EPL> lo[U], hi[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int hh = min(h + u, h1 - 1);
-            const TI *x = hh < p.H ? q + hh * p.qsh : k + (hh - p.H) * p.ksh;
-            lo[u] = load_piece<TI, EPL, ONCE>(x);
-            hi[u] = load_piece<TI, EPL, ONCE>(x + D / 2);
-        }
+    for (int u = 0; u < U; ++u) {
+        const int h = min(h0 + u, heads - 1);
+        const TI *x = h < p.H ? q + h * p.qsh : k + (h - p.H) * p.ksh;
+        lo[u] = load_piece<TI, EPL, ONCE>(x);
+        hi[u] = load_piece<TI, EPL, ONCE>(x + D / 2);
+    }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int hh = h + u;
-            if (hh >= h1) break;
-            float a[EPL], c[EPL];
-            widen<TI, EPL>(lo[u], a);
-            widen<TI, EPL>(hi[u], c);
+    for (int u = 0; u < U; ++u) {
+        const int h = h0 + u;
+        if (h >= heads) break;
+        float a[EPL], c[EPL];
+        widen<TI, EPL>(lo[u], a);
+        widen<TI, EPL>(hi[u], c);
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) turn(a[e], c[e], cs[e], turned[e]);
-            TO *y = hh < p.H ? qo + hh * p.oqsh : ko + (hh - p.H) * p.oksh;
-            store_piece<TO, EPL, ONCE>(narrowed<TO, EPL>(a), y);
-            store_piece<TO, EPL, ONCE>(narrowed<TO, EPL>(c), y + D / 2);
-        }
+        for (int e = 0; e < EPL; ++e) turn(a[e], c[e], cs[e], turned[e]);
+        TO *y = h < p.H ? qo + h * p.oqsh : ko + (h - p.H) * p.oksh;
+        store_piece<TO, EPL, ONCE>(narrowed<TO, EPL>(a), y);
+        store_piece<TO, EPL, ONCE>(narrowed<TO, EPL>(c), y + D / 2);
     }
 }
+
+// Rows are not kept in the caches from 192 MB on, read and written, where a lane's
+// halves lie in different lines of 128 bytes: 131 MB 14.5 us kept and 17.7 not, 262 MB
+// (float32) 46.8 and 45.7, 537 MB 95 and 89; bf16 at D = 64 (halves of 64 bytes) 537 MB
+// 97 and 108.
+constexpr int64_t kKeepBytes = 192 << 20;
 
 template <typename TI, typename TO, int D>
 hipError_t launch_d(RotateParams p, hipStream_t stream) {
     using R = HalfRow<TI, D>;
     const int heads = p.H + p.Hk;
-    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI;
-    p.splits = (int)std::clamp<int64_t>(8192 / tiles, 1, (heads + U - 1) / U);
-    p.per = ((heads + p.splits - 1) / p.splits + U - 1) / U * U;
-    p.splits = (heads + p.per - 1) / p.per;
-    p.by_splits = Divisor(p.splits);
-    const int64_t groups = (tiles * p.splits + WAVES - 1) / WAVES;
-    if (groups >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
-    return launch_kernel(rotate_kernel<TI, TO, D, false>, dim3((unsigned)groups), dim3(64 * WAVES), stream, p);
+    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = (heads + U - 1) / U;
+    const int64_t blocks = (tiles * groups + WAVES - 1) / WAVES;
+    if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
+    const bool heads_first = p.H > 0 ? p.qsh < p.qsn : p.ksh < p.ksn;
+    p.order = WaveOrder(heads_first, (uint32_t)tiles, (uint32_t)groups);
+    constexpr bool kWide = D / 2 * sizeof(TI) >= 128;
+    const bool once = kWide && (int64_t)p.rows * heads * D * (int64_t)(sizeof(TI) + sizeof(TO)) > kKeepBytes;
+    return launch_kernel(once ? rotate_kernel<TI, TO, D, kWide> : rotate_kernel<TI, TO, D, false>, dim3((unsigned)blocks),
+                         dim3(64 * WAVES), stream, p);
 }
 
 template <typename TI, typename TO>
