@@ -375,7 +375,8 @@ def run(state):
     if c["kind"] == "store":
         if own:
             pa.pi_attn_paged_store(s["k"], s["v"], s["kp"], s["vp"], s["table"], s["start"], s["count"], k_exp=s["ke"],
-                                   v_exp=s["ve"], freq=s["freq"], pos=s["pos"], sections=s["sections"])
+                                   v_exp=s["ve"], freq=s["freq"], pos=s["pos"] if c["rot"] else None,
+                                   sections=s["sections"])
         else:
             _store(c, s)
         r = {"k": s["kp"], "v": s["vp"]}
@@ -392,8 +393,8 @@ def run(state):
         if own:
             out = pa.pi_attn_decode_step_paged(
                 s["len_in"], s["q"], s["k"], s["v"], s["kp"], s["vp"], s["table"], s["gate"], c["k"], c["pi"],
-                k_exp=s["ke"], v_exp=s["ve"], freq=s["freq"], pos=s["pos"], sections=s["sections"],
-                logit_clamp=c["clamp"], len_out=length, lse=lse)
+                k_exp=s["ke"], v_exp=s["ve"], freq=s["freq"], pos=s["pos"] if c["rot"] else None,
+                sections=s["sections"], logit_clamp=c["clamp"], len_out=length, lse=lse)
         else:
             out, lse, length = _decode(c, s)
         r = {"out": out, "lse": lse, "len": length, "k": s["kp"], "v": s["vp"]}
