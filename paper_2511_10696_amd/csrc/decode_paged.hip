@@ -28,13 +28,10 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(PagedStepParams p) {
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t head = blockIdx.x, heads = (int64_t)p.S * p.H;
     const int t = p.len_in[s];
-    if (!has_place(p.pages, s, t)) {
-        if (tid < D) ((T *)p.out)[head * D + tid] = (T)NAN;
-        if (p.lse && tid == 0) p.lse[head] = NAN;
-        if (p.len_out && h == 0 && tid == 0) p.len_out[s] = t;
-        return;
-    }
-    const int n = ranges_of(p, t - window_lo(t, p.k));
+    const bool in_reach = t >= 0 && t < (int64_t)p.pages.page * p.pages.max_pages;
+    // (looked at behind the parts, which need not wait for it)
+    const int entry = in_reach ? p.pages.table[(int64_t)s * p.pages.max_pages + p.pages.by_page.div(t)] : -1;
+    const int n = in_reach ? ranges_of(p, t - window_lo(t, p.k)) : 0;
     float M = -INFINITY, L = 0.0f, o[EPL] = {};
     for (int x = w; x < n; x += WAVES * U) {
         float2 ml[U];
@@ -70,6 +67,12 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(PagedStepParams p) {
         s_l[w] = L;
     }
     __syncthreads();
+    if (page_named(p.pages, entry) < 0) {
+        if (tid < D) ((T *)p.out)[head * D + tid] = (T)NAN;
+        if (p.lse && tid == 0) p.lse[head] = NAN;
+        if (p.len_out && h == 0 && tid == 0) p.len_out[s] = t;
+        return;
+    }
     if (tid < D) {
         float top = -INFINITY, sum = 0.0f, out = 0.0f;
 #pragma unroll

@@ -28,28 +28,33 @@ constexpr int U = 2;   // heads of a wavefront, their keys' and values' loads in
 
 // What a lane does for its row, all heads alike.
 struct Place {
-    bool there;       // the row has a place in the cache
+    bool wanted;      // its position is within the table's reach, and the row in the count
     uint32_t s, i;    // sequence and row of k and v
     int at;           // its position
-    int64_t first;    // cache row of head 0; head h's is h * page further on
-};
+    int entry;        // the table's, not looked at before page() is asked
+    uint32_t slot;
 
-template <int RPI>
-__device__ inline bool place(const PagedRowsParams &p, uint32_t tile, int rg, Place &a) {
-    const uint32_t r = tile * RPI + rg;
-    if (r >= p.rows) return false;
-    a.s = p.by_n.div(r);
-    a.i = r - a.s * p.n;
-    const int64_t at = (int64_t)a.i + (p.start ? p.start[a.s] : 0);
-    const Pages &g = p.pages;
-    a.there = at >= 0 && at < (int64_t)g.page * g.max_pages && (!p.count || (int)a.i < p.count[a.s]);
-    a.at = a.there ? (int)at : 0;
-    const uint32_t slot = g.by_page.div(a.at);
-    const int entry = a.there ? g.table[(int64_t)a.s * g.max_pages + slot] : -1;
-    a.there = a.there && entry >= 0 && entry < g.n_pages;
-    a.first = (int64_t)(a.there ? entry : 0) * p.Hk * g.page + (a.at - slot * g.page);
-    return true;
-}
+    template <int RPI>
+    __device__ bool find(const PagedRowsParams &p, uint32_t tile, int rg) {
+        const uint32_t r = tile * RPI + rg;
+        if (tile >= p.order.tiles || r >= p.rows) return false;
+        s = p.by_n.div(r);
+        i = r - s * p.n;
+        const int64_t pos = (int64_t)i + (p.start ? p.start[s] : 0);
+        const Pages &g = p.pages;
+        wanted = pos >= 0 && pos < (int64_t)g.page * g.max_pages && (!p.count || (int)i < p.count[s]);
+        at = wanted ? (int)pos : 0;
+        slot = g.by_page.div(at);
+        entry = wanted ? g.table[(int64_t)s * g.max_pages + slot] : -1;
+        return true;
+    }
+    __device__ int page(const Pages &g) const { return entry >= 0 && entry < g.n_pages ? entry : -1; }
+    // Cache row of head 0; head h's is h * page further on.
+    __device__ int64_t first(const PagedRowsParams &p) const {
+        const Pages &g = p.pages;
+        return (int64_t)max(page(g), 0) * p.Hk * g.page + (at - slot * g.page);
+    }
+};
 
 // LD, SD: what is loaded, or stored, is not kept in the caches.
 template <typename T, bool QUANT, int D, bool LD, bool SD>
@@ -61,8 +66,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_store_kernel(PagedRowsParams
     uint32_t tile, group;
     p.order.place(wave, tile, group);
     Place a;
-    if (tile >= p.order.tiles || !place<R::RPI>(p, tile, rg, a)) return;
-    if (!a.there) return;   // a row's lanes alike
+    if (!a.find<R::RPI>(p, tile, rg) || !a.wanted) return;   // a row's lanes alike
     const int h0 = (int)group * U;
     const int64_t from = a.s * p.sb + a.i * p.sn + sub * EPL;
     const T *k = (const T *)p.k + from, *v = (const T *)p.v + from;
@@ -87,10 +91,12 @@ __global__ __launch_bounds__(64 * WAVES) void paged_store_kernel(PagedRowsParams
         }
     }
     const Pages &g = p.pages;
+    if (a.page(g) < 0) return;
+    const int64_t first = a.first(p);
     // A row's halves into head h's pages, as these hold them.
     auto put = [&](const Piece<T, EPL> &lo, const Piece<T, EPL> &hi, bool turns, int h, void *pages, uint8_t *exps)
         __attribute__((always_inline)) {
-        const int64_t row = a.first + (int64_t)h * g.page;
+        const int64_t row = first + (int64_t)h * g.page;
         float x[EPL], y[EPL];
         if (QUANT || turns) {
             widen<T, EPL>(lo, x);
@@ -140,7 +146,9 @@ __global__ __launch_bounds__(64 * WAVES) void paged_load_kernel(PagedRowsParams 
     uint32_t tile, group;
     p.order.place(wave, tile, group);
     Place a;
-    if (tile >= p.order.tiles || !place<R::RPI>(p, tile, rg, a)) return;
+    if (!a.find<R::RPI>(p, tile, rg)) return;
+    const bool there = a.page(p.pages) >= 0;
+    const int64_t first = a.first(p);
     const int h0 = (int)group * U;
     const int64_t to = a.s * p.sb + a.i * p.sn + sub * EPL;
     T *k = (T *)p.k + to, *v = (T *)p.v + to;
@@ -166,8 +174,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_load_kernel(PagedRowsParams 
         kb[u] = vb[u] = 127;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[u][j] = Piece<ST, EPL>{};   // absent rows: zeros, in codes too
-        if (a.there) {
-            const int64_t row = a.first + (int64_t)min(h0 + u, p.Hk - 1) * g.page;
+        if (there) {
+            const int64_t row = first + (int64_t)min(h0 + u, p.Hk - 1) * g.page;
             x[u][0] = load_piece<ST, EPL, LD>(kp + row * D);
             x[u][1] = load_piece<ST, EPL, LD>(kp + row * D + D / 2);
             x[u][2] = load_piece<ST, EPL, LD>(vp + row * D);

@@ -25,11 +25,6 @@ __device__ inline int page_of(const Pages &g, int64_t s, uint32_t slot) {
     return page_named(g, g.table[s * g.max_pages + slot]);
 }
 
-// Whether sequence s can take a row at t.
-__device__ inline bool has_place(const Pages &g, int64_t s, int t) {
-    return t >= 0 && t < (int64_t)g.page * g.max_pages && page_of(g, s, g.by_page.div(t)) >= 0;
-}
-
 // Rows of the longest window that the cache can hold, the new row apart.
 inline int64_t longest_window(const PagedStepParams &p) {
     return std::min<int64_t>(p.k, (int64_t)p.pages.page * p.pages.max_pages - 1);
