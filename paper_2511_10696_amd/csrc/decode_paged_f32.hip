@@ -98,6 +98,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
     const float *const kn = (const float *)p.k_new + ((int64_t)s * p.Hk + hk) * D;
     const float *const vn = (const float *)p.v_new + ((int64_t)s * p.Hk + hk) * D;
     const bool rotary = p.r.freq != nullptr;
+    const Angle angle = angle_of(p.r, min(tid, D / 2), s, 0, t);   // of pair tid
     float q[QN][4], gate[QN];
 #pragma unroll
     for (int j = 0; j < QN; ++j) {
@@ -106,7 +107,6 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
         gate[j] = p.gate[s * p.gss + (hk * G + g0 + jj) * p.gsh];
     }
     look_up(w);
-    if (rotary && tid < D / 2) s_cs[tid] = cos_sin_of(p.r, tid, s, 0, t);
     if (place < 0) {
         if (part) return;
         for (int i = tid; i < nq * D; i += 64 * WAVES) ((float *)p.out)[first_head * D + i] = NAN;
@@ -136,6 +136,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
     load(w, ra);
     look_up(w + WAVES);
 
+    if (rotary && tid < D / 2) s_cs[tid] = cos_sin(angle.pos, angle.freq);
     // Four elements of a row from 4 * sub on turned; `row`: where the others of their
     // pairs are.
     auto turned = [&](const float *row, float (&f)[4]) __attribute__((always_inline)) {

@@ -123,6 +123,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
     // What does not depend on the pages is asked for first: the queries (a k-step by
     // each wavefront; the other elements of their pairs too) and the gate.
     const bool rotary = p.r.freq != nullptr;
+    const Angle angle = angle_of(p.r, min(tid, D / 2), s, 0, t);   // of pair tid
     // N elements of a new row in the working type.
     auto wide = [&](const T *from, auto &f) __attribute__((always_inline)) {
         constexpr int N = sizeof(f) / 4, E = 16 / (int)sizeof(T);
@@ -198,7 +199,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         return row >= 0 ? byte : 127;
     };
     look_up(w);
-    if (rotary && tid < D / 2) s_cs[tid] = cos_sin_of(p.r, tid, s, 0, t);
     if (place < 0) {
         if (part) return;
         for (int i = tid; i < nq * D; i += 64 * WAVES) ((T *)p.out)[first_head * D + i] = (T)NAN;
@@ -216,6 +216,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         load(pages.v, row, vr);
     }
 
+    if (rotary && tid < D / 2) s_cs[tid] = cos_sin(angle.pos, angle.freq);
     // Elements from `dim` on turned, `o` the other elements of their pairs.
     auto turned = [&](auto &f, const auto &o, int dim) __attribute__((always_inline)) {
 #pragma unroll

@@ -30,11 +30,20 @@ __device__ inline float2 cos_sin(int pos, float freq) {
     return make_float2(c, s);
 }
 
-// Of pair i at row n of sequence b, which is position `at` of the sequence.
-__device__ inline float2 cos_sin_of(const Rotary &r, int i, int64_t b, int64_t n, int at) {
-    if (i >= r.pairs) return make_float2(1.0f, 0.0f);
+// What pair i at row n of sequence b is turned by, once asked for (0 beyond the last
+// pair), where the row is position `at` of its sequence.
+struct Angle {
+    float freq;
+    int pos;
+};
+__device__ inline Angle angle_of(const Rotary &r, int i, int64_t b, int64_t n, int at) {
+    if (!r.freq || i >= r.pairs) return Angle{0.0f, 0};
     const int axis = i < r.end0 ? 0 : i < r.end1 ? 1 : 2;
-    return cos_sin(r.pos ? r.pos[axis * r.psa + b * r.psb + n * r.psn] : at, r.freq[i]);
+    return Angle{r.freq[i], r.pos ? r.pos[axis * r.psa + b * r.psb + n * r.psn] : at};
+}
+__device__ inline float2 cos_sin_of(const Rotary &r, int i, int64_t b, int64_t n, int at) {
+    const Angle a = angle_of(r, i, b, n, at);
+    return cos_sin(a.pos, a.freq);
 }
 
 // A pair (a, b) turned; pairs from r.pairs on are not touched, whatever they hold.
