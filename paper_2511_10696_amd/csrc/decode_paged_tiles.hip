@@ -156,7 +156,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
     // last range the new one and the partner.
     const int first = lo + range * len;
     const int nwin = in_reach ? min(len, t - first) : 0;
-    const bool last = first + nwin == t;
+    const bool last = in_reach && first + nwin == t;
     const int jp = partner_of(t, p.k, p.pi);
     const int nrows = nwin + (last ? jp >= 0 ? 2 : 1 : 0);
     const int ntiles = (nrows + TILE - 1) / TILE;

@@ -115,6 +115,7 @@ STEP = [(dict(dtype=3), EUNSUP), (dict(D=80), EUNSUP), (dict(S=-1), EINVAL), (di
         (dict(gate=2), EINVAL), (dict(gs=(-1, 1)), EINVAL), (dict(lse=2), EINVAL), (dict(ke=1), EINVAL), (dict(ve=1), EINVAL),
         (dict(n=(30, 3, 0)), EINVAL), (dict(pos=2), EINVAL), (dict(ps=(-1, 0), pos=4), EINVAL),
         (dict(page=1 << 16, max=1 << 15), EUNSUP), (dict(S=1 << 14, H=1 << 10, Hk=1), EUNSUP),
+        (dict(pages=1 << 20, page=1 << 11), EUNSUP), (dict(pages=1 << 20, page=1 << 10, Hk=6), EUNSUP),
         (dict(page=1024, max=64, k=1 << 20), EINVAL), (dict(page=1024, max=64, k=1 << 20, work=8), EINVAL)]
 
 
@@ -136,6 +137,8 @@ def test_workspace():
     assert ws(bf, 0, 8, 8, 128, 16, 10000, 1 << 20) == 0
     # the cache's reach bounds the window
     assert ws(bf, 1, 8, 8, 128, 16, 10000, 1 << 30) == ws(bf, 1, 8, 8, 128, 16, 10000, 160000)
+    # fewer than 2^32 threads of 256 a part
+    assert ws(bf, 1, 1 << 20, 1, 64, 16, 10000, 1 << 20) <= (1 << 23) * 66
     for bad in ((bf, -1, 8, 8, 128, 16, 10, 5), (bf, 1, 8, 3, 128, 16, 10, 5), (bf, 1, 8, 8, 96, 16, 10, 5),
                 (bf, 1, 8, 8, 128, 0, 10, 5), (bf, 1, 8, 8, 128, 16, 0, 5), (bf, 1, 8, 8, 128, 16, 10, -1)):
         with pytest.raises(pa.PiAttnError):

@@ -153,6 +153,30 @@ def test_lengths_without_a_place(device, quantised):
     run(cache, lens, *new_rows(6, 4, 2, 64, BF, 2), 20, 30)
 
 
+@pytest.mark.parametrize("dt,quantised", [(F, False), (BF, False), (BF, True)])
+def test_empty_windows_past_the_reach(device, dt, quantised):
+    """k = 0: the window of a length past the table's reach begins where it ends."""
+    cache = Cache(4, 2, 64, 8, 5, dt, quantised, 1)
+    run(cache, [40, 41, 2 ** 31 - 1, 39], *new_rows(4, 4, 2, 64, dt, 2), 0, 0)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+def test_pools_past_32_bits(device, dt):
+    """Rows more than 2^32 bytes into the pool; rows of it past 2^31 are refused."""
+    page, Hk, D, es = 64, 8, 128, 2 if dt == BF else 4
+    n_pages = (1 << 32) // (page * Hk * D * es) + 40
+    kp, vp = (torch.zeros(n_pages, Hk, page, D, dtype=dt, device="cuda") for _ in range(2))
+    small = Cache(2, Hk, D, page, 4, dt, False, 3)
+    far = n_pages - small.k.shape[0]
+    kp[far:], vp[far:] = small.k, small.v
+    q, k, v, gate = new_rows(2, 16, Hk, D, dt, 4)
+    lens = i32(200, 255)
+    want = pa.pi_attn_decode_step_paged(lens, q, k, v, small.k, small.v, small.table, gate, 150, 180)
+    got = pa.pi_attn_decode_step_paged(lens, q, k, v, kp, vp, (small.table + far).contiguous(), gate, 150, 180)
+    assert torch.equal(got, want) and torch.equal(kp[far:], small.k) and torch.equal(vp[far:], small.v)
+    assert not kp[:far].any() and not vp[:far].any()
+
+
 LONG = [
     # H, Hk, D, page, rows, dtype, quantised, k, pi, clamp, lengths: windows split over work-groups
     (8, 8, 128, 16, 5000, BF, False, 4999, 0, 0.0, [4990, 7, 1025]),
