@@ -111,16 +111,16 @@ hipError_t launch_join(const PagedStepParams &p, hipStream_t stream) {
 // Where a few (s, key head) have long windows, these are split: three work-groups a
 // CU, from 128 rows each (a tile for each wavefront) to 1024, which balances sequences of
 // unlike lengths.  A split costs the join's launch, 4 us.  us, whole and split, bf16, D =
-// 128: 8 (s, key head) of 512 rows 13.0 and 14.8, of 1024 15.6 and 14.4; 64 of 1024 18.6
-// and 18.7; 128 of 1024 20.2 and 23.5, of 4096 53 and 43; 256 of 1024 27.3 and 33.9, of
-// 2048 38.5 and 42.2; D = 64, 8 of 2048 16.0 and 10.6.  Ranges of a window of 65536, 8 of
-// them: of 256 rows 58, 512 53, 1024 51, 2048 57.  At most 4096 work-groups where the
-// lengths turn out to be short (these have none of the ranges but the first), and fewer
-// than 2^32 threads.
+// 128, four query heads each: 8 (s, key head) of 512 rows 10.6 and 12.6, of 1024 14.7 and
+// 12.8, of 2040 22.1 and 12.0; 64 of 1024 17.7 and 17.9, of 2040 27.5 and 20.9; 128 of 1024
+// 19.0 and 22.3, of 2000 to 4095 51.5 and 41.8; 256 of 1024 27.0 and 32.0, of 2040 45.2 and
+// 50.6.  Ranges of 8 windows of 65536: of 256 rows 55.9, 512 51.9, 1024 50.3, 2048 51.7.
+// At most 4096 work-groups where the lengths turn out to be short (these have none of the
+// ranges but the first), and fewer than 2^32 threads.
 void plan_decode_paged(PagedStepParams &p) {
     const int64_t n = (int64_t)p.S * p.Hk, rows = longest_window(p);
     p.parts = p.range = 0;
-    if (n >= 4096 || rows <= (n <= 192 ? 1024 : 2048)) return;
+    if (n >= 4096 || rows <= (n <= 16 ? 768 : n <= 192 ? 1024 : 2048)) return;
     p.range = (int)std::clamp<int64_t>((rows * n / 768 + 127) & ~(int64_t)127, 128, 1024);
     p.parts = (int)std::min({(rows + p.range - 1) / p.range, 4096 / n, (int64_t)(1 << 23) / ((int64_t)p.S * p.H)});
     if (p.parts < 2) p.parts = p.range = 0;

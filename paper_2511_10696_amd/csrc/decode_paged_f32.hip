@@ -6,6 +6,12 @@
 // and of values a chunk; the next chunk's are under way while one is worked on.  Every
 // row read serves QN queries.  Each group of lanes that covers a row keeps a softmax of
 // its own (nothing is exchanged from row to row); they are merged at the end.
+//
+// What bounds it: HBM where a key head has one query (64 sequences of 16 heads, 250 to 400
+// rows, D = 128: 314 MB in 52 us, 6.0 TB/s); the multiply-adds and the sums across lanes
+// where it has more (16 sequences of 1000 to 1990 rows, 8 key heads of four: 197 MB in 48
+// us, 4.1 TB/s).  Rows a chunk ahead: 34 -> 22 us (16 sequences of 16 heads, 800 to 990
+// rows, D = 64).
 #include <algorithm>
 
 #include "paged_step.h"

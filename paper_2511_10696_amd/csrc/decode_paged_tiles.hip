@@ -21,8 +21,16 @@
 // Precision.  The products take bf16: cached rows are that, or e4m3, whose codes and
 // scales together are bf16 numbers.  A query (turned, not rounded) and a weight are
 // split into TERMS bf16 numbers, two (off by 2^-17) where the result is bf16, three
-// (2^-24) where it is float32: the matrix cores have time to spare, a row of 256
-// bytes costs 32 query columns 16 KFLOP.
+// (2^-24) where it is float32: the matrix cores have time to spare (16 KFLOP a row of 256
+// bytes for 16 columns of two terms; busy 8% of the time).
+//
+// What bounds it: HBM with many long windows (64 sequences of 2000 to 8191 rows, 8 key
+// heads of four queries, bf16, D = 128: 1.34 GB in 217 us, 6.2 TB/s, with the join 222;
+// one wavefront after the other on rows by fused multiply-adds 414).  With few, the chain
+// of one wavefront: length, page, rows (one microsecond each) and 1.3 us a tile (one user
+// of 32 heads, 512 rows: 11.3 us).  Eight wavefronts of a work-group instead of four, where
+// it has its CU to itself: 11.3 and 13.3 us there; 256 work-groups of 1024 rows 26.6 and
+// 29.0.  Sixteen with tiles of 16 rows: 12.0 and 26.6.
 #include <algorithm>
 #include "bf16_rows.h"
 #include "paged_step.h"
