@@ -623,13 +623,16 @@ int64_t pi_attn_paged_workspace(int32_t dtype, int32_t S, int32_t H, int32_t Hk,
  *   work         device float32, 16-byte aligned, of pi_attn_paged_workspace(dtype,
  *                S, H, Hk, D, page, max_pages, k) elements; may be NULL when that is 0.
  * A length outside [0, page * max_pages), or whose position has no page: NaN for that
- * sequence's outputs, the cache untouched, len_out[s] = len_in[s].  Long windows of a
- * few (s, key head) are split over work-groups, in two launches; the sums are taken in
- * a fixed order either way, and which kernels run depends on the sizes alone.
+ * sequence's outputs, the cache untouched, len_out[s] = len_in[s].  Keys and values of
+ * W_t that are not finite may give NaN (in bf16 and e4m3 pages, where a weight is a sum of
+ * two or three terms, an infinite value does).  Long windows of a few (s, key head) are
+ * split over work-groups, in two launches; the sums are taken in a fixed order either way,
+ * and which kernels run depends on the sizes alone.
  * Errors: EINVAL (null pointer, negative size, H not a multiple of Hk, misalignment, one
  * of k_exp and v_exp without the other, n0 + n1 + n2 > D/2, a null or misaligned work
  * that is needed), EUNSUPPORTED (D not 64/128, unknown dtype, page * max_pages above
- * 2^31 - 4097, S*H of 2^24 and more), EHIP (launch refused).
+ * 2^31 - 4097, n_pages * page * Hk of 2^31 and more, S*H of 2^24 and more), EHIP (launch
+ * refused).
  */
 int pi_attn_decode_step_paged(int32_t dtype, int32_t S, int32_t H, int32_t Hk, int32_t D, int32_t n_pages, int32_t page,
                               int32_t max_pages, int32_t k, int32_t pi, const int32_t *len_in, int32_t *len_out,

@@ -108,22 +108,22 @@ hipError_t launch_join(const PagedStepParams &p, hipStream_t stream) {
 
 }  // namespace
 
-// Where a few (s, key head) have long windows, these are split: three work-groups a
-// CU, from 128 rows each (a tile for each wavefront) to 1024, which balances sequences of
-// unlike lengths.  A split costs the join's launch, 4 us.  us, whole and split, bf16, D =
-// 128, four query heads each: 8 (s, key head) of 512 rows 10.6 and 12.6, of 1024 14.7 and
-// 12.8, of 2040 22.1 and 12.0; 64 of 1024 17.7 and 17.9, of 2040 27.5 and 20.9; 128 of 1024
-// 19.0 and 22.3, of 2000 to 4095 51.5 and 41.8; 256 of 1024 27.0 and 32.0, of 2040 45.2 and
-// 50.6.  Ranges of 8 windows of 65536: of 256 rows 55.9, 512 51.9, 1024 50.3, 2048 51.7.
-// At most 4096 work-groups where the lengths turn out to be short (these have none of the
-// ranges but the first), and fewer than 2^32 threads.
+// Where a few (s, key head) can have long windows, these are split, by the lengths that
+// they turn out to have (range_len), which balances sequences of unlike lengths too.  A
+// split costs the join's launch, 4 us.  us, whole and split, bf16, D = 128, four query
+// heads each: 8 (s, key head) of 512 rows 10.6 and 12.6, of 1024 14.7 and 12.8, of 2040 22.1
+// and 12.0; 64 of 1024 17.7 and 17.9, of 2040 27.5 and 20.9; 128 of 1024 19.0 and 22.3, of
+// 2000 to 4095 51.5 and 41.8; 256 of 1024 27.0 and 32.0, of 2040 45.2 and 50.6.  Ranges of
+// 8 windows of 65536: of 256 rows 55.9, 512 51.9, 1024 50.3, 2048 51.7.  At most some 4096
+// work-groups (those of ranges that a window has not end at once), and fewer than 2^32
+// threads.
 void plan_decode_paged(PagedStepParams &p) {
     const int64_t n = (int64_t)p.S * p.Hk, rows = longest_window(p);
-    p.parts = p.range = 0;
+    p.parts = 0;
     if (n >= 4096 || rows <= (n <= 16 ? 768 : n <= 192 ? 1024 : 2048)) return;
-    p.range = (int)std::clamp<int64_t>((rows * n / 768 + 127) & ~(int64_t)127, 128, 1024);
-    p.parts = (int)std::min({(rows + p.range - 1) / p.range, 4096 / n, (int64_t)(1 << 23) / ((int64_t)p.S * p.H)});
-    if (p.parts < 2) p.parts = p.range = 0;
+    const int64_t parts = std::min({std::max(768 / n + 1, (rows + 1023) / 1024), (rows + 127) / 128, 4096 / n,
+                                    (int64_t)(1 << 23) / ((int64_t)p.S * p.H)});
+    if (parts > 1) p.parts = (int)parts;
 }
 
 hipError_t launch_decode_paged(const PagedStepParams &p, bool bf16, hipStream_t stream) {

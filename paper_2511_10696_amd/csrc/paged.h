@@ -73,11 +73,10 @@ struct PagedStepParams {
     float scale, clamp;
     void *out;                      // [S][H][D]
     float *lse;                     // [S][H] or nullptr
-    // Parts from ranges of the windows, at least `range` rows each and at most `parts`
-    // of a window (0: not split): for part x at[x][s * H + h] the weighted values [D],
-    // then (max, sum) in log2 units.
+    // Parts from ranges of the windows, at most `parts` of one (0: not split): for part x
+    // at[x][s * H + h] the weighted values [D], then (max, sum) in log2 units.
     float *part_o, *part_ml;
-    int range, parts;
+    int parts;
 };
 
 hipError_t launch_rotate(const RotateParams &p, bool bf16_in, bool bf16_out, hipStream_t stream);

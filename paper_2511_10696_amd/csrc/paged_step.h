@@ -37,11 +37,12 @@ inline bool read_once(const PagedStepParams &p, int q_groups, int element_bytes)
     return q_groups == 1 && 2 * (int64_t)p.S * p.Hk * longest_window(p) * p.D * element_bytes > kKeepBytes;
 }
 
-// Rows of a range, and ranges, of a window of n rows in a split step: p.range, more
-// where that would be more than p.parts ranges; whole steps of 128 rows.
+// Rows of a range, and ranges, of a window of n rows in a split step: for three
+// work-groups a CU if all windows are alike, from 128 rows (a tile for each wavefront) to
+// 1024, more where that would be more than p.parts ranges; whole steps of 128 rows.
 __device__ inline int range_len(const PagedStepParams &p, int n) {
-    const int even = (int)((((int64_t)n + p.parts - 1) / p.parts + 127) & ~(int64_t)127);
-    return max(p.range, even);
+    const int64_t fill = (int64_t)n * (p.S * p.Hk) / 768, even = ((int64_t)n + p.parts - 1) / p.parts;
+    return (int)((max(min(fill, (int64_t)1024), max(even, (int64_t)128)) + 127) & ~(int64_t)127);
 }
 __device__ inline int ranges_of(const PagedStepParams &p, int n) {
     const int len = range_len(p, n);

@@ -50,6 +50,42 @@ def test_chunked_prompt_then_tokens(device, D, page, kw, pi):
     assert torch.equal(kc, kt) and torch.equal(vc, v) and lens.tolist() == [N, N]
 
 
+def test_captured_run(device):
+    """Rotation, store, load and a split step in a graph, replayed with new data and eager calls between: as the eager run."""
+    S, H, Hk, D, n = 2, 8, 2, 64, 1500
+    g = torch.Generator().manual_seed(9)
+    freq = frequencies(32).cuda()
+    gate = torch.zeros(H, device="cuda")
+    k, v = (torch.empty(S, Hk, n, D, dtype=BF, device="cuda") for _ in range(2))
+    q1, k1, v1 = (torch.empty(S, h, D, dtype=BF, device="cuda") for h in (H, Hk, Hk))
+    count = torch.tensor([n, 900], dtype=torch.int32, device="cuda")
+    cache = Cache(S, Hk, D, 16, 100, BF, False, 2)
+
+    def one():
+        kt, _ = pa.pi_attn_rotate(k, None, None, freq)
+        pa.pi_attn_paged_store(kt, v, cache.k, cache.v, cache.table, count=count)
+        out = pa.pi_attn_decode_step_paged(count, q1, k1, v1, cache.k, cache.v, cache.table, gate, 1400, 1450, freq=freq)
+        return (kt, out, *pa.pi_attn_paged_load(cache.k, cache.v, cache.table, n + 1, count=count + 1))
+
+    def fill():
+        for x in (k, v, q1, k1, v1):
+            x.copy_(torch.randn(x.shape, generator=g))
+
+    fill()
+    one()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = one()
+    for _ in range(3):
+        fill()
+        graph.replay()
+        torch.cuda.synchronize()
+        got_now = [x.clone() for x in got]
+        for a, b in zip(got_now, one()):
+            assert torch.equal(a, b)
+
+
 def test_streaming_with_pages_given_back(device):
     """A window that moves on: pages behind it are given to the sequence's next positions, and nothing changes."""
     H, D, page, kw = 3, 64, 8, 30
