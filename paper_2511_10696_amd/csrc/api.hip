@@ -118,7 +118,8 @@ const char *pi_attn_strerror(int status) {
         case PI_ATTN_EINVAL: return "invalid argument (null pointer, negative size or stride, misalignment)";
         case PI_ATTN_EUNSUPPORTED:
             return "unsupported configuration (head dimension must be 64 or 128; dtype f32/bf16; bf16: "
-                   "(k + 256) rows of keys, (2k + 256) bidirectional, must span under 2 GiB)";
+                   "(k + 256) rows of keys, (2k + 256) bidirectional, must span under 2 GiB; paged caches: fewer than "
+                   "2^31 positions of a sequence and rows of the pool)";
         case PI_ATTN_EHIP: return "HIP runtime refused the launch";
         case PI_ATTN_ESCRATCH:
             return "problem too large for the no-allocation backward's fixed row-term array (B*H*N > 4194304)";

@@ -32,6 +32,7 @@
 // it has its CU to itself: 11.3 and 13.3 us there; 256 work-groups of 1024 rows 26.6 and
 // 29.0.  Sixteen with tiles of 16 rows: 12.0 and 26.6.
 #include <algorithm>
+
 #include "bf16_rows.h"
 #include "paged_step.h"
 
@@ -199,12 +200,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
             r[i] = ONCE ? ld16_once(from) : ld16(from);
         }
     };
-    // Scale bytes: of the keys in the first TILE lanes, of the values in the next.
+    // Scale bytes: of the keys in the first TILE lanes, of the values in the next (of rows
+    // that are not there whatever, and not looked at here: no wait).
     auto load_bytes = [&](int row) __attribute__((always_inline)) -> int {
         if constexpr (!Q) return 0;
-        const uint8_t *const from = lane < TILE ? pages.k_exp : pages.v_exp;
-        const int byte = from[max(row, 0)];
-        return row >= 0 ? byte : 127;
+        return (lane < TILE ? pages.k_exp : pages.v_exp)[max(row, 0)];
     };
     look_up(w);
     if (place < 0) {
