@@ -212,6 +212,24 @@ def test_large_pools(device, quantised):
         assert torch.equal(ko, k) and torch.equal(vo, v)
 
 
+def test_rows_past_32_bits(device):
+    """Rows more than 2^31 elements into k and v: as a call of those rows alone."""
+    n, D, page = (1 << 31) // 64 + 500, 64, 256
+    k = torch.zeros(1, 1, n, D, dtype=BF, device="cuda")
+    v = torch.zeros(1, 1, n, D, dtype=BF, device="cuda")
+    k[:, :, -90:], v[:, :, -90:] = rows(1, 1, 90, D, BF, "shnd", 2)
+    count = n // page + 1
+    pages = [torch.full((count, 1, page, D), 3.0, dtype=BF, device="cuda") for _ in range(2)]
+    table = torch.arange(count, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    freq = frequencies(32).cuda()
+    pa.pi_attn_paged_store(k, v, *pages, table, freq=freq)
+    kt, _ = pa.pi_attn_rotate(k[:, :, -90:].contiguous(), None, torch.arange(n - 90, n, dtype=torch.int32, device="cuda"), freq)
+    del k
+    ko, vo = pa.pi_attn_paged_load(*pages, table, n)
+    assert torch.equal(ko[:, :, -90:], kt) and torch.equal(vo, v) and not ko[:, :, :-90].any()
+    assert (pages[0].view(-1, D)[n % page:page] == 3.0).all()   # behind the last row, in the last page
+
+
 def test_on_a_given_stream_and_python_path(device, monkeypatch):
     S, Hk, n, D = 2, 3, 40, 64
     k, v = rows(S, Hk, n, D, BF, "snhd", 2)

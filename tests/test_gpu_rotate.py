@@ -179,6 +179,17 @@ def test_attention_depends_on_differences(device):
     assert (outs[0] - outs[1]).abs().max() <= 64 * 2.0 ** -19 * 8 * 2 / 8 * 5
 
 
+def test_past_32_bits(device):
+    """Heads and positions more than 2^31 elements into q: as a call of those rows alone."""
+    H, N, D = 3, (1 << 31) // (2 * 64) + 1000, 64
+    q = torch.zeros(1, H, N, D, dtype=BF, device="cuda")
+    q[:, :, -70:] = data(1, H, 70, D, BF, "bhnd", 1)
+    freq = frequencies(32).cuda()
+    want, _ = pa.pi_attn_rotate(q[:, :, -70:].contiguous(), None, torch.arange(N - 70, N, dtype=torch.int32, device="cuda"), freq)
+    got, _ = pa.pi_attn_rotate(q, None, None, freq)
+    assert torch.equal(got[:, :, -70:], want) and not got[:, :, :-70].any()
+
+
 def test_on_a_given_stream(device):
     q, k = data(2, 3, 500, 64, BF, "bhnd", 1), data(2, 3, 500, 64, BF, "bhnd", 2)
     pos, freq = positions(1, 2, 500, 5, 3), frequencies(32).cuda()
