@@ -342,16 +342,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
             }
         }
         // A lane's scores are of rows 4g + i and 16 + 4g + i.
-        float d[8], unit = CLAMP ? 1.0f : c2;   // of d, in log2 units
+        float d[8];   // logits, log2 units
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = sc[i >> 2][i & 3];
+        for (int i = 0; i < 8; ++i) d[i] = CLAMP ? sc[i >> 2][i & 3] : sc[i >> 2][i & 3] * c2;
         if (CLAMP || special) {
-            unit = 1.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const bool partner = special && 16 * (i >> 2) + 4 * g + (i & 3) == new_r + 1;
                 d[i] = CLAMP ? clamped_logit(d[i] * p.scale + (partner ? fb.partner : fb.local), p.clamp) * kLog2e
-                             : d[i] * c2 + (partner ? fb.partner * kLog2e : 0.0f);
+                             : d[i] + (partner ? fb.partner * kLog2e : 0.0f);
             }
         }
         if (!whole) {
@@ -362,7 +361,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         float top = d[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) top = fmaxf(top, d[i]);
-        top *= unit;
         if (__builtin_amdgcn_ballot_w64(top > m + kTau)) {
             top = query_max(top);
             const float m_new = top > m + kTau ? top : m;
@@ -376,7 +374,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         bf16x8 pb[TERMS];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(d[i], unit, -mu));
+            const float pr = weight(d[i], mu);
             l += pr;
             __bf16 terms[TERMS];
             split<TERMS>(pr, terms);

@@ -12,6 +12,14 @@ namespace pi_attn {
 
 constexpr float kTau = 8.0f;   // a running maximum is raised in steps above this, log2 units
 
+// A row's weight 2^(d - m), d its logit as the maximum m has seen it.  Were the product that
+// d comes from left unrounded here, the largest row's weight would be 2^r, r the rounding
+// of m: 256 and more from logits of 2^32 on, which overflows or leaves no row a weight.
+__device__ inline float weight(float d, float m) {
+#pragma clang fp contract(off)
+    return __builtin_amdgcn_exp2f(d - m);
+}
+
 template <typename ST>
 inline constexpr bool kQuantised = false;
 template <>
