@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
         for (int j = 0; j < QN; ++j) {
             if (!entered) continue;
             m[j] = d[j];
-            l[j] = __builtin_amdgcn_exp2f(d[j] - (d[j] == -INFINITY ? 0.0f : d[j]));   // 1, or NaN
+            l[j] = weight(d[j], d[j] == -INFINITY ? 0.0f : d[j]);   // 1, 0 or NaN
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[j][e] = l[j] * vf[e];
         }
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(64 * WAVES) void decode_paged_f32_kernel(PagedStepP
             to_f32<float>(r.v[c], vf);
 #pragma unroll
             for (int j = 0; j < QN; ++j) {
-                const float pr = __builtin_amdgcn_exp2f(sc[c][j] - (m[j] == -INFINITY ? 0.0f : m[j]));
+                const float pr = weight(sc[c][j], m[j] == -INFINITY ? 0.0f : m[j]);
                 l[j] += pr;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[j][e] += pr * vf[e];

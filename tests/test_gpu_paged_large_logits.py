@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
 
 
-@pytest.mark.parametrize("dtype,quantised", [(BF, False), (BF, True), (F, True)])
+@pytest.mark.parametrize("dtype,quantised", [(BF, False), (BF, True), (F, True), (F, False)])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("S,rows,kw,pi", [(5, 200, 150, 170), (2, 3000, 2500, 2600)])   # whole windows; split ones
 @pytest.mark.parametrize("top", ["window", "partner", "new"])
