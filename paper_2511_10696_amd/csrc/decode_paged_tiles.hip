@@ -76,6 +76,23 @@ __device__ inline void split(float x, __bf16 (&t)[TERMS]) {
     }
 }
 
+// The same of a query's element past bf16's largest number: no infinity for a finite one, and no
+// second term beside an infinity or NaN (their difference is NaN, and a clamp makes an infinite
+// logit finite).
+constexpr float kLargestBf16 = 0x1.fep127f;
+
+template <int TERMS>
+__device__ inline void split_large(float x, __bf16 (&t)[TERMS]) {
+    const bool finite = fabsf(x) < INFINITY;
+    t[0] = (__bf16)(finite ? fminf(fmaxf(x, -kLargestBf16), kLargestBf16) : x);
+    x = finite ? x - (float)t[0] : 0.0f;
+#pragma unroll
+    for (int i = 1; i < TERMS; ++i) {
+        t[i] = (__bf16)x;
+        x -= (float)t[i];
+    }
+}
+
 // Orders a wavefront's own LDS accesses: its lanes read what others wrote.
 __device__ inline void lds_order() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -279,12 +296,22 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
     if (w < L::STEPS) {
         if (rotary) turned(q_own, q_other, q_dim);
         bf16x8 q[TERMS];
+        auto split_row = [&](auto &&one) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            __bf16 terms[TERMS];
-            split<TERMS>(c < nq ? q_own[e] : 0.0f, terms);
+            for (int e = 0; e < 8; ++e) {
+                __bf16 terms[TERMS];
+                one(c < nq ? q_own[e] : 0.0f, terms);
 #pragma unroll
-            for (int i = 0; i < TERMS; ++i) q[i][e] = terms[i];
+                for (int i = 0; i < TERMS; ++i) q[i][e] = terms[i];
+            }
+        };
+        float most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(q_own[e]));
+        if (__builtin_amdgcn_ballot_w64(most > kLargestBf16)) {
+            split_row([](float x, __bf16 (&t)[TERMS]) { split_large<TERMS>(x, t); });
+        } else {
+            split_row([](float x, __bf16 (&t)[TERMS]) { split<TERMS>(x, t); });
         }
 #pragma unroll
         for (int i = 0; i < TERMS; ++i) s_q[i][w][lane] = q[i];
