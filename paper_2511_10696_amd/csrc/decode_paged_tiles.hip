@@ -354,7 +354,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         lds_order();   // the tile before has been read
 #pragma unroll
         for (int i = 0; i < L::LOADS; ++i) put(kr[i], i * L::R::RPI + rg, scale_of(i, 0));
-        if (special && new_r >= 0 && rg == 0) put(s_new[0][sub], new_r, e4m3_scale(s_new_bytes[0]));
+        if (special && new_r >= 0) {
+            lds_order();   // over what its place held, by other lanes
+            if (rg == 0) put(s_new[0][sub], new_r, e4m3_scale(s_new_bytes[0]));
+        }
         if (more) load(pages.k, next, kr);
         lds_order();
         f32x4 sc[2] = {f32x4{}, f32x4{}};
@@ -411,13 +414,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 3 : 2) void decode_tiles_k
         lds_order();   // the keys have been read
 #pragma unroll
         for (int i = 0; i < L::LOADS; ++i) put(vr[i], i * L::R::RPI + rg, scale_of(i, 1));
-        if (!whole && row < 0) {   // rows that are not there may hold anything
-            constexpr int LANES = 64 / TILE;   // of a row
-            unsigned char *const to = lds + lane % TILE * L::PITCH + lane / TILE * (2 * D / LANES);
+        if (!whole) {   // rows that are not there may hold anything
+            lds_order();   // over what other lanes wrote
+            if (row < 0) {
+                constexpr int LANES = 64 / TILE;   // of a row
+                unsigned char *const to = lds + lane % TILE * L::PITCH + lane / TILE * (2 * D / LANES);
 #pragma unroll
-            for (int i = 0; i < 2 * D / LANES; i += 16) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 2 * D / LANES; i += 16) *reinterpret_cast<uint4 *>(to + i) = make_uint4(0, 0, 0, 0);
+            }
         }
-        if (special && new_r >= 0 && rg == 0) put(s_new[1][sub], new_r, e4m3_scale(s_new_bytes[1]));
+        if (special && new_r >= 0) {
+            lds_order();
+            if (rg == 0) put(s_new[1][sub], new_r, e4m3_scale(s_new_bytes[1]));
+        }
         if (more) load(pages.v, next, vr);
         lds_order();
         const int vrow = 4 * g + ((lane >> 2) & 3), qd = lane & 3;
