@@ -2,7 +2,10 @@
 // caches' rows and of the decode step over them.
 #pragma once
 
+#include <algorithm>
+
 #include "cached.h"
+#include "kernels.h"
 #include "rotary.h"
 
 namespace pi_attn {
@@ -12,16 +15,32 @@ namespace pi_attn {
 struct WaveOrder {
     bool heads_first;
     uint32_t tiles, groups;
+    uint32_t first;                 // wavefront, of several launches
     Divisor by_inner;
     WaveOrder() = default;
-    WaveOrder(bool hf, uint32_t t, uint32_t g) : heads_first(hf), tiles(t), groups(g), by_inner(hf ? g : t) {}
-    // Tile and group of wavefront `wave`; tile is past the last one for those without work.
+    WaveOrder(bool hf, uint32_t t, uint32_t g) : heads_first(hf), tiles(t), groups(g), first(0), by_inner(hf ? g : t) {}
+    // Tile and group of a launch's wavefront; tile is past the last one for those without work.
     __device__ void place(uint32_t wave, uint32_t &tile, uint32_t &group) const {
+        wave += first;
         const uint32_t outer = by_inner.div(wave), inner = wave - outer * (heads_first ? groups : tiles);
         tile = heads_first || outer >= groups ? (heads_first ? outer : tiles) : inner;
         group = heads_first ? inner : outer;
     }
 };
+
+// Launches `kernel` on work-groups of WAVES wavefronts, as often as it takes: a launch has fewer
+// than 2^32 threads.
+template <int WAVES, typename P>
+hipError_t launch_in_order(void (*kernel)(P), P &p, hipStream_t stream) {
+    constexpr int64_t kMost = (int64_t)1 << 23;
+    const int64_t blocks = ((int64_t)p.order.tiles * p.order.groups + WAVES - 1) / WAVES;
+    hipError_t e = hipSuccess;
+    for (int64_t b = 0; e == hipSuccess && b < blocks; b += kMost) {
+        p.order.first = (uint32_t)(b * WAVES);
+        e = launch_kernel(kernel, dim3((unsigned)std::min(blocks - b, kMost)), dim3(64 * WAVES), stream, p);
+    }
+    return e;
+}
 
 // Rows of q [B][H][N][D] and k [B][Hk][N][D] turned, forward or back.
 struct RotateParams {

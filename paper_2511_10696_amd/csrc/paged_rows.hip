@@ -206,18 +206,15 @@ template <typename T, bool QUANT, int D>
 hipError_t launch_d(PagedRowsParams p, bool store, hipStream_t stream) {
     using R = HalfRow<T, D>;
     constexpr int NARROW = QUANT ? 1 : (int)sizeof(T);   // bytes of an element in the pages
-    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = (p.Hk + U - 1) / U;
-    const int64_t blocks = (tiles * groups + WAVES - 1) / WAVES;
-    if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
+    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = ((int64_t)p.Hk + U - 1) / U;
     p.order = WaveOrder(p.sh < p.sn, (uint32_t)tiles, (uint32_t)groups);
     const bool once = 2 * (int64_t)p.rows * p.Hk * D * (int64_t)(sizeof(T) + NARROW) > kKeepBytes;
     constexpr bool kStoreLd = D / 2 * sizeof(T) >= 128, kLoadLd = D / 2 * NARROW >= 128;
-    const dim3 grid((unsigned)blocks), block(64 * WAVES);
     if (store)
-        return launch_kernel(once ? paged_store_kernel<T, QUANT, D, kStoreLd, true> : paged_store_kernel<T, QUANT, D, false, false>,
-                             grid, block, stream, p);
-    return launch_kernel(once ? paged_load_kernel<T, QUANT, D, kLoadLd, true> : paged_load_kernel<T, QUANT, D, false, false>, grid,
-                         block, stream, p);
+        return launch_in_order<WAVES>(once ? paged_store_kernel<T, QUANT, D, kStoreLd, true>
+                                           : paged_store_kernel<T, QUANT, D, false, false>, p, stream);
+    return launch_in_order<WAVES>(once ? paged_load_kernel<T, QUANT, D, kLoadLd, true>
+                                       : paged_load_kernel<T, QUANT, D, false, false>, p, stream);
 }
 
 template <typename T>

@@ -86,15 +86,12 @@ template <typename TI, typename TO, int D>
 hipError_t launch_d(RotateParams p, hipStream_t stream) {
     using R = HalfRow<TI, D>;
     const int heads = p.H + p.Hk;
-    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = (heads + U - 1) / U;
-    const int64_t blocks = (tiles * groups + WAVES - 1) / WAVES;
-    if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;   // 2^32 threads
+    const int64_t tiles = ((int64_t)p.rows + R::RPI - 1) / R::RPI, groups = ((int64_t)heads + U - 1) / U;
     const bool heads_first = p.H > 0 ? p.qsh < p.qsn : p.ksh < p.ksn;
     p.order = WaveOrder(heads_first, (uint32_t)tiles, (uint32_t)groups);
     constexpr bool kWide = D / 2 * sizeof(TI) >= 128;
     const bool once = kWide && (int64_t)p.rows * heads * D * (int64_t)(sizeof(TI) + sizeof(TO)) > kKeepBytes;
-    return launch_kernel(once ? rotate_kernel<TI, TO, D, kWide> : rotate_kernel<TI, TO, D, false>, dim3((unsigned)blocks),
-                         dim3(64 * WAVES), stream, p);
+    return launch_in_order<WAVES>(once ? rotate_kernel<TI, TO, D, kWide> : rotate_kernel<TI, TO, D, false>, p, stream);
 }
 
 template <typename TI, typename TO>
