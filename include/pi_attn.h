@@ -520,13 +520,15 @@ int pi_attn_gate_grad_per_head(int32_t B, int32_t H, int32_t N, const float *dga
  *                value, negative ones too), or NULL: n, on every axis.
  *   freq         device float32 [n0 + n1 + n2], radians a position; NULL: nothing
  *                is turned.
- *   q_out, k_out through (oqsb, ...), (oksb, ...), each at least D where its extent
- *                is more than 1.  Either may be its input itself (same pointer,
- *                type and strides); otherwise nothing may overlap.
+ *   q_out, k_out through (oqsb, ...), (oksb, ...).  Of the extents above 1 the least
+ *                stride is at least D and each other one at least the next smaller
+ *                one times its extent (any order in memory, slices too).  Either may
+ *                be its input itself (same pointer, type and strides); otherwise
+ *                nothing may overlap, which is looked at for equal pointers alone.
  * Errors: EINVAL (null or misaligned pointer of a non-empty tensor, negative size or
- * stride, rows of an output that meet, an output at its input with other strides or
- * type, n0 + n1 + n2 > D/2, B*N*(H + Hk) of 2^31 and more), EUNSUPPORTED (D not
- * 64/128, unknown dtype), EHIP (launch refused).
+ * stride, other strides of an output, an output at its input with other strides or
+ * type, at the other input or at the other output, n0 + n1 + n2 > D/2, B*N*(H + Hk)
+ * of 2^31 and more), EUNSUPPORTED (D not 64/128, unknown dtype), EHIP (launch refused).
  */
 int pi_attn_rotate(int32_t dtype, int32_t out_dtype, int32_t B, int32_t H, int32_t Hk, int32_t N, int32_t D, int32_t back,
                    const void *q, int64_t qsb, int64_t qsh, int64_t qsn, const void *k, int64_t ksb, int64_t ksh,
@@ -579,9 +581,10 @@ int pi_attn_paged_store(int32_t dtype, int32_t S, int32_t Hk, int32_t D, int32_t
  * no row.  bf16 rows can go into pi_attn_forward_shard as the rows that a later chunk
  * of the prompt attends.
  *   Arguments    as pi_attn_paged_store; every row of k and v [S][Hk][n][D] is written
- *                (through sb, sh, sn, each at least D where its extent is more than
- *                1).  Pages in dtype are copied bit by bit.
- * Errors: as pi_attn_paged_store, and EINVAL for rows of k and v that meet.
+ *                (through sb, sh, sn: of the extents above 1 the least stride is at
+ *                least D and each other one at least the next smaller one times its
+ *                extent).  Pages in dtype are copied bit by bit.
+ * Errors: as pi_attn_paged_store, and EINVAL for other strides and for k at v.
  */
 int pi_attn_paged_load(int32_t dtype, int32_t S, int32_t Hk, int32_t D, int32_t n, int32_t n_pages, int32_t page,
                        int32_t max_pages, const void *k_pages, const void *v_pages, const uint8_t *k_exp,

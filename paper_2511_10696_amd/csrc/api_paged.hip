@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/pi_attn.h"
 #include "checks.h"
 #include "paged.h"
@@ -13,9 +15,20 @@ namespace {
 
 bool strides_ok(int es, int64_t a, int64_t b, int64_t c) { return stride16(a, es) && stride16(b, es) && stride16(c, es); }
 
-// Rows that a call writes lie apart.
+// Rows that a call writes lie apart: by rising stride, the dimensions of more than one row are
+// nested in each other, as any order of them in memory and any slice of it is.
 bool apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t D) {
-    return !((n0 > 1 && s0 < D) || (n1 > 1 && s1 < D) || (n2 > 1 && s2 < D));
+    struct Dim {
+        int64_t n, s;
+    } dims[3] = {{n0, s0}, {n1, s1}, {n2, s2}};
+    std::sort(dims, dims + 3, [](const Dim &a, const Dim &b) { return a.s < b.s; });
+    int64_t least = D;
+    for (const Dim &d : dims) {
+        if (d.n <= 1) continue;
+        if (d.s < least) return false;
+        least = d.n > INT64_MAX / d.s ? INT64_MAX : d.n * d.s;
+    }
+    return true;
 }
 
 // The rotation of rows of D elements; freq == nullptr or no pairs: none.
@@ -80,7 +93,7 @@ int paged_rows(bool store, int32_t dtype, int32_t S, int32_t Hk, int32_t D, int3
     if ((int64_t)S * Hk * n == 0) return PI_ATTN_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v) || !strides_ok(es, sb, sh, sn)) return PI_ATTN_EINVAL;
     if ((start && !aligned4(start)) || (count && !aligned4(count))) return PI_ATTN_EINVAL;
-    if (!store && !apart(S, sb, Hk, sh, n, sn, D)) return PI_ATTN_EINVAL;
+    if (!store && (k == v || !apart(S, sb, Hk, sh, n, sn, D))) return PI_ATTN_EINVAL;
     status = check_pages(n_pages, page, max_pages, table, k_pages, v_pages, k_exp, v_exp, p.pages);
     if (status != PI_ATTN_OK) return status;
     p.S = S; p.Hk = Hk; p.n = n; p.D = D;
@@ -144,6 +157,7 @@ int pi_attn_rotate(int32_t dtype, int32_t out_dtype, int32_t B, int32_t H, int32
         if (!apart(B, oksb, Hk, oksh, N, oksn, D)) return PI_ATTN_EINVAL;
         if (k == k_out && (es != eo || ksb != oksb || ksh != oksh || ksn != oksn)) return PI_ATTN_EINVAL;
     }
+    if (H > 0 && Hk > 0 && (q_out == k_out || q_out == k || k_out == q)) return PI_ATTN_EINVAL;
     p.B = B; p.H = H; p.Hk = Hk; p.N = N; p.D = D;
     p.q = q; p.k = k; p.q_out = q_out; p.k_out = k_out;
     p.qsb = qsb; p.qsh = qsh; p.qsn = qsn; p.ksb = ksb; p.ksh = ksh; p.ksn = ksn;
