@@ -504,9 +504,11 @@ int pi_attn_gate_grad_per_head(int32_t B, int32_t H, int32_t N, const float *dga
  * axis a is turned by the angle pos_a * freq[i]:
  *   y_i       = x_i cos - x_(i + D/2) sin
  *   y_(i+D/2) = x_i sin + x_(i + D/2) cos.
- * Pairs from n0 + n1 + n2 <= D/2 on stay as they are, bit by bit.  Angles are formed
- * in 64 bits from the float32 frequencies, the rest is fp32 with one rounding at
- * the end.
+ * Pairs from n0 + n1 + n2 <= D/2 on stay as they are, bit by bit.  There is this one
+ * pairing, for fewer than D/2 pairs too: a model made for another (2i and 2i + 1; i and
+ * i + P inside the first 2P elements; axes interleaved) needs the rows of its query and
+ * key projections permuted.  Angles are formed in 64 bits from the float32 frequencies,
+ * the rest is fp32 with one rounding at the end.
  *
  * pi_attn_rotate -- q and k turned by their positions, or back.
  *   dtype, out_dtype   of q, k and of q_out, k_out.
@@ -579,7 +581,8 @@ int pi_attn_paged_store(int32_t dtype, int32_t S, int32_t Hk, int32_t D, int32_t
  * pi_attn_paged_load -- rows of a paged cache in sequence and in dtype: row i < n of
  * k and v is position start[s] + i, and zeros where i >= count[s] or that position has
  * no row.  bf16 rows can go into pi_attn_forward_shard as the rows that a later chunk
- * of the prompt attends.
+ * of the prompt attends, where there are as many key heads as query heads and the
+ * sequences are equally far.
  *   Arguments    as pi_attn_paged_store; every row of k and v [S][Hk][n][D] is written
  *                (through sb, sh, sn: of the extents above 1 the least stride is at
  *                least D and each other one at least the next smaller one times its
@@ -613,7 +616,8 @@ int64_t pi_attn_paged_workspace(int32_t dtype, int32_t S, int32_t H, int32_t Hk,
  *                dimension.
  *   n_pages, page, max_pages, table, k_pages, v_pages, k_exp, v_exp   the cache;
  *                position t of every key head is overwritten, nothing else is written.
- *                The page of position t must belong to sequence s alone.
+ *                The page of position t must belong to sequence s alone, and no other
+ *                row of W_t lie at position t's place in it.
  *   k, pi        window radius and partner period.
  *   len_in       device int32 [S]: rows so far.
  *   len_out      optional device int32 [S]: receives len_in[s] + 1; must not overlap

@@ -1005,7 +1005,8 @@ def pi_attn_rotate(q, k, pos, freq, sections=None, dtype=None, q_out=None, k_out
     three whole numbers that sum to P (time, height and width: the first pairs
     belong to axis 0, the next to axis 1, ...); None: one axis.  pos: int32
     [axes, B, N], for one axis [B, N] or [N] too, any strides; None: 0..N-1.
-    Angles are formed in 64 bits.  Returns (q, k) turned, contiguous and in
+    (There is this one pairing: a model made for another needs the rows of its query and
+    key projections permuted.)  Angles are formed in 64 bits.  Returns (q, k) turned, contiguous and in
     ``dtype`` (the inputs'), or in q_out, k_out; either may be its input itself.
     """
     return _rotate(q, k, pos, freq, sections, dtype, q_out, k_out, stream, False, "pi_attn_rotate")

@@ -115,8 +115,8 @@ hipError_t launch_join(const PagedStepParams &p, hipStream_t stream) {
 // and 12.0; 64 of 1024 17.7 and 17.9, of 2040 27.5 and 20.9; 128 of 1024 19.0 and 22.3, of
 // 2000 to 4095 51.5 and 41.8; 256 of 1024 27.0 and 32.0, of 2040 45.2 and 50.6.  Ranges of
 // 8 windows of 65536: of 256 rows 55.9, 512 51.9, 1024 50.3, 2048 51.7.  At most some 4096
-// work-groups (those of ranges that a window has not end at once), and fewer than 2^32
-// threads.
+// work-groups (those of ranges that a window has not end at once) for each group of query
+// heads of a key head (16, of float32 pages 8), and fewer than 2^32 threads.
 void plan_decode_paged(PagedStepParams &p) {
     const int64_t n = (int64_t)p.S * p.Hk, rows = longest_window(p);
     p.parts = 0;

@@ -1,5 +1,6 @@
 // decode_paged_tiles.hip -- the decode step over a paged cache on the matrix
 // cores: pages in bf16 or e4m3, up to 16 query heads of a key head at a time.
+// (The new row and the partner are rows of the tiles, behind the window's last.)
 //
 // A work-group is a sequence, a key head, up to 16 of its query heads and a range
 // of the window; its wavefronts take tiles of 32 rows in turn, each with a running
@@ -21,11 +22,11 @@
 // Precision.  The products take bf16: cached rows are that, or e4m3, whose codes and
 // scales together are bf16 numbers.  A query (turned, not rounded) and a weight are
 // split into TERMS bf16 numbers, two (off by 2^-17) where the result is bf16, three
-// (2^-24) where it is float32: the matrix cores have time to spare (16 KFLOP a row of 256
+// (2^-24) where it is float32: the matrix cores have time to spare (8 KFLOP a row of 256
 // bytes for 16 columns of two terms; busy 8% of the time).
 //
 // What bounds it: HBM with many long windows (64 sequences of 2000 to 8191 rows, 8 key
-// heads of four queries, bf16, D = 128: 1.34 GB in 217 us, 6.2 TB/s, with the join 222;
+// heads of four queries, bf16, D = 128: 1.34 GB in 218 us, 6.1 TB/s, with the join 224;
 // one wavefront after the other on rows by fused multiply-adds 414).  With few, the chain
 // of one wavefront: length, page, rows (one microsecond each) and 1.3 us a tile (one user
 // of 32 heads, 512 rows: 11.3 us).  Eight wavefronts of a work-group instead of four, where
@@ -51,7 +52,9 @@ struct Tiles {
     static constexpr int STEPS = D / 32;             // k-steps of the scores
     static constexpr int DB = D / 16;                // 16-dim output blocks
     // LDS rows, padded by 16 bytes: the reads of the scores take one 16-byte piece of 16
-    // rows, the transpose reads 32 bytes of them, and both meet all banks equally.
+    // rows, the transpose reads 32 bytes of them, and both meet all banks equally.  Writes of
+    // codes do not (a lane's two pieces lie 32 bytes from its neighbour's): of the LDS cycles
+    // 42% are conflicts there, 20% with bf16 pages.
     static constexpr int PITCH = 2 * D + 16;
     static constexpr int BYTES = TILE * PITCH;
 };

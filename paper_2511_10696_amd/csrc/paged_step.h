@@ -46,7 +46,7 @@ inline bool read_once(const PagedStepParams &p, int q_groups, int element_bytes)
 }
 
 // Rows of a range, and ranges, of a window of n rows in a split step: for three
-// work-groups a CU if all windows are alike, from 128 rows (a tile for each wavefront) to
+// work-groups a CU (of each group of query heads) if all windows are alike, from 128 rows (a tile for each wavefront) to
 // 1024, more where that would be more than p.parts ranges; whole steps of 128 rows.
 __device__ inline int range_len(const PagedStepParams &p, int n) {
     const int64_t fill = (int64_t)n * (p.S * p.Hk) / 768, even = ((int64_t)n + p.parts - 1) / p.parts;

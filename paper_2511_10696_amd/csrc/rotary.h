@@ -17,10 +17,11 @@ struct Rotary {
     int64_t psa, psb, psn;          // its element strides: axis, sequence, row
 };
 
-// cos and sin of pos * freq.  The angle is formed in turns and in 64 bits, where
-// |pos| < 2^31 leaves an error below 2^-24 of a turn for |freq| <= 1 (2^-34 up to a
-// million positions); in 32 bits a position of 2^20 would be off by a hundredth
-// of a turn.
+// cos and sin of pos * freq.  The angle is formed in turns and in 64 bits.  For |freq| <= 1
+// and |pos| < 2^31 it is off by less than 2^-23 of a turn: 2^-25.5 by the constant (off by
+// 2^-56.5), 2^-25 by its product with freq, 2^-25 by the turns (up to 2^28.4); up to a
+// million positions 2^-34.  In 32 bits a position of 2^20 would be off by a hundredth of a
+// turn.
 __device__ inline float2 cos_sin(int pos, float freq) {
     constexpr double kTurns = 0.15915494309189535;   // 1 / (2 pi)
     const double turns = (double)pos * ((double)freq * kTurns);
